@@ -506,6 +506,48 @@ int ec_mask_process_threshold(int P, size_t S, double fraction, uint64_t* host_m
 int ec_threshold_segments(const uint32_t* contrib_count, size_t S, uint32_t need, uint32_t* ready_segments,
                           ec_stream_t stream);
 
+/* ------------------------------------------------------------------------- *
+ * Operators of a language model whose gradients the collectives combine.
+ * Additions of this library (the paper has no counterpart): the first layer
+ * (embedding), products grouped by expert, and a distillation loss.  All are
+ * stateless: one call = the launches it names on `stream`, no allocation, no
+ * synchronisation.  Element types are EC_F32 or EC_BF16 (EC_ERR_UNSUPPORTED
+ * otherwise); sums, softmax statistics and products are fp32, rounded once
+ * (to nearest even) when an output is bf16.  Results repeat bit for bit.
+ * Strides are in elements, from one row to the next, at least the row length
+ * (EC_ERR_INVALID otherwise); elements between rows are neither read nor written.
+ * Outputs must not overlap inputs unless a call says so.
+ * ------------------------------------------------------------------------- */
+typedef enum {
+    EC_INDEX_32 = 0, /* int32 */
+    EC_INDEX_64 = 1  /* int64 */
+} ec_index_t;
+
+/* Embedding lookup with scaling: out[t] = scale * table[tokens[t]], t < T.
+ * A token outside [0, V) - padding is usually -1 - gives a row of zeros.
+ *   table   device [V][D], rows table_stride apart;   out  device [T][D], rows out_stride apart
+ *   tokens  device int32 or int64 [T]
+ * Limits: 1 <= V, T < 2^31 - 1 (T = 0: nothing is done), 1 <= D <= 2^24.  Rows that start on 16-byte boundaries and are
+ * a multiple of eight (bf16 table) or four (fp32) elements long take the vector path.  One launch. */
+int ec_embed_lookup(const void* table, size_t V, size_t D, size_t table_stride, ec_dtype_t table_dtype, const void* tokens,
+                    ec_index_t index, size_t T, float scale, void* out, size_t out_stride, ec_dtype_t out_dtype,
+                    ec_stream_t stream);
+
+/* Its gradient: grad[v] = scale * sum of dout[t] over the t with tokens[t] = v, as a dense [V][D] array - a rank buffer for
+ * ec_allreduce_apply / ec_allreduce_ssp_apply.  Tokens outside [0, V) and tokens equal to skip_token (a padding id whose row
+ * is not trained; a negative value names none) give nothing.
+ *   accumulate  0: all of grad is written, rows without a token with zeros;  nonzero: the sums are added to grad, rows
+ *               without a token are neither read nor written (gradient accumulation over micro-batches).
+ *   workspace   device, ec_embed_grad_workspace_bytes(T, V, D) bytes, 256-byte aligned (EC_ERR_CAPACITY otherwise); its
+ *               contents need no initialisation and are garbage afterwards.  Calls that may run at the same time need one each.
+ * The tokens are sorted (a stable radix sort), then sorted tokens and table rows are walked together in equal shares; a row
+ * is summed in fp32 in ascending t inside a share and its shares in ascending order, so the bits do not depend on timing.
+ * Limits as ec_embed_lookup; T = 0 is allowed.  T + V < 2^31. */
+size_t ec_embed_grad_workspace_bytes(size_t T, size_t V, size_t D);
+int ec_embed_grad(const void* dout, size_t dout_stride, ec_dtype_t dout_dtype, const void* tokens, ec_index_t index, size_t T,
+                  size_t V, size_t D, float scale, int64_t skip_token, int accumulate, void* grad, size_t grad_stride,
+                  ec_dtype_t grad_dtype, void* workspace, size_t workspace_bytes, ec_stream_t stream);
+
 /* ------------------------------------------------------------------------- */
 const char* ec_strerror(int code);
 /* The cudaError_t of the last failed CUDA call on this thread (0 if none). */

@@ -64,6 +64,9 @@ SYMBOLS = {
     "ec_mask_data_fraction": (_i, [_i, _sz, C.c_double, _vp]),
     "ec_mask_process_threshold": (_i, [_i, _sz, C.c_double, _vp, C.POINTER(_i)]),
     "ec_threshold_segments": (_i, [_vp, _sz, C.c_uint32, _vp, _vp]),
+    "ec_embed_lookup": (_i, [_vp, _sz, _sz, _sz, _i, _vp, _i, _sz, C.c_float, _vp, _sz, _i, _vp]),
+    "ec_embed_grad_workspace_bytes": (_sz, [_sz, _sz, _sz]),
+    "ec_embed_grad": (_i, [_vp, _sz, _i, _vp, _i, _sz, _sz, _sz, C.c_float, C.c_int64, _i, _vp, _sz, _i, _vp, _sz, _vp]),
     "ec_strerror": (C.c_char_p, [_i]),
     "ec_last_cuda_error": (_i, []),
     "ec_version": (_i, []),
@@ -360,3 +363,61 @@ class MatrixFactorization:
             self.destroy()
         except Exception:
             pass
+
+
+# ---- operators of a language model: 2-D device tensors whose rows are contiguous (any row stride) -----------------
+
+_REAL = {torch.float32: F32, torch.bfloat16: BF16}
+_INDEX = {torch.int32: 0, torch.int64: 1}
+
+
+def _rows(t: torch.Tensor, what: str):
+    """(rows, columns, row stride, dtype code) of a 2-D tensor."""
+    code = _REAL.get(t.dtype)
+    if code is None:
+        raise EcError(ERR_UNSUPPORTED, f"{what}: fp32 or bf16 expected")
+    if t.dim() != 2 or not t.is_cuda:
+        raise EcError(ERR_INVALID, f"{what}: a 2-D device tensor expected")
+    n, d = t.shape
+    s0, s1 = t.stride()
+    if s1 != 1 and d > 1:
+        raise EcError(ERR_INVALID, f"{what}: elements of a row must be adjacent")
+    return n, d, s0 if n > 1 else max(s0, d), code
+
+
+def _ids(t: torch.Tensor, what: str) -> int:
+    code = _INDEX.get(t.dtype)
+    if code is None:
+        raise EcError(ERR_UNSUPPORTED, f"{what}: int32 or int64 expected")
+    if not t.is_cuda or not t.is_contiguous():
+        raise EcError(ERR_INVALID, f"{what}: a contiguous device tensor expected")
+    return code
+
+
+def embed_lookup(table, tokens, out, scale: float = 1.0, stream=None) -> None:
+    """ec_embed_lookup: out[t] = scale * table[tokens[t]], zeros for a token outside the table."""
+    V, D, ts, td = _rows(table, "embed_lookup table")
+    T, Do, os_, od = _rows(out, "embed_lookup out")
+    idx = _ids(tokens, "embed_lookup tokens")
+    if Do != D or tokens.numel() != T:
+        raise EcError(ERR_INVALID, "embed_lookup: out must be [number of tokens][row length of the table]")
+    _check(lib().ec_embed_lookup(table.data_ptr(), V, D, ts, td, tokens.data_ptr(), idx, T, scale, out.data_ptr(), os_, od,
+                                 _stream(stream)), "ec_embed_lookup")
+
+
+def embed_grad_workspace_bytes(T: int, V: int, D: int) -> int:
+    """ec_embed_grad_workspace_bytes: device bytes embed_grad needs for T tokens and a [V][D] table."""
+    return lib().ec_embed_grad_workspace_bytes(T, V, D)
+
+
+def embed_grad(dout, tokens, grad, workspace, scale: float = 1.0, skip_token: int = -1, accumulate: bool = False,
+               stream=None) -> None:
+    """ec_embed_grad: grad[v] (+)= scale * sum of dout[t] over tokens[t] = v; workspace is a device uint8 tensor."""
+    T, D, ds, dd = _rows(dout, "embed_grad dout")
+    V, Dg, gs, gd = _rows(grad, "embed_grad grad")
+    idx = _ids(tokens, "embed_grad tokens")
+    if Dg != D or tokens.numel() != T:
+        raise EcError(ERR_INVALID, "embed_grad: dout must be [number of tokens][row length of grad]")
+    _check(lib().ec_embed_grad(dout.data_ptr(), ds, dd, tokens.data_ptr(), idx, T, V, D, scale, skip_token,
+                               1 if accumulate else 0, grad.data_ptr(), gs, gd, workspace.data_ptr(), workspace.numel(),
+                               _stream(stream)), "ec_embed_grad")

@@ -1,0 +1,95 @@
+// Typed vector accesses of the language-model operators: W consecutive elements of fp32 or bf16 (raw bits) as fp32 in
+// registers, rounded to nearest even once when they are stored.
+#pragma once
+
+#include <cuda_bf16.h>
+
+#include "ec_common.cuh"
+
+namespace ec {
+
+struct bf16_t { uint16_t bits; };
+
+__device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+__device__ __forceinline__ uint32_t pack2_bf16(float lo, float hi) {
+    uint32_t u;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(u) : "f"(hi), "f"(lo));
+    return u;
+}
+
+// Raw bits of W elements: what a thread keeps in flight (a bf16 vector takes half the registers of its values).
+template <class T, int W> struct raw_vec { uint32_t u[sizeof(T) * W >= 4 ? sizeof(T) * W / 4 : 1]; };
+
+template <class T, int W>
+__device__ __forceinline__ raw_vec<T, W> load_raw(const T* p) {          // read once: not kept in L1
+    raw_vec<T, W> r;
+    constexpr int B = (int)sizeof(T) * W;
+    if constexpr (B == 16) {
+        const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
+        r.u[0] = v.x; r.u[1] = v.y; r.u[2] = v.z; r.u[3] = v.w;
+    } else if constexpr (B == 8) {
+        const uint2 v = __ldcs(reinterpret_cast<const uint2*>(p));
+        r.u[0] = v.x; r.u[1] = v.y;
+    } else if constexpr (B == 4) {
+        r.u[0] = __ldcs(reinterpret_cast<const uint32_t*>(p));
+    } else {
+        static_assert(B == 2, "one bf16");
+        r.u[0] = __ldcs(reinterpret_cast<const uint16_t*>(p));
+    }
+    return r;
+}
+template <class T, int W>
+__device__ __forceinline__ void unpack(const raw_vec<T, W>& r, float (&x)[W]) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int i = 0; i < W; ++i) x[i] = __uint_as_float(r.u[i]);
+    } else if constexpr (W == 1) {
+        x[0] = __uint_as_float(r.u[0] << 16);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) { x[2 * i] = bf16_lo(r.u[i]); x[2 * i + 1] = bf16_hi(r.u[i]); }
+    }
+}
+template <class T, int W>
+__device__ __forceinline__ void load_vec(const T* p, float (&x)[W]) { unpack<T, W>(load_raw<T, W>(p), x); }
+
+template <class T, int W>
+__device__ __forceinline__ void store_vec(T* p, const float (&x)[W]) {   // written once: not kept in L1
+    if constexpr (sizeof(T) == 4) {
+        if constexpr (W % 4 == 0) {
+#pragma unroll
+            for (int i = 0; i < W / 4; ++i)
+                __stcs(reinterpret_cast<float4*>(p) + i, make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < W; ++i) __stcs(reinterpret_cast<float*>(p) + i, x[i]);
+        }
+    } else {
+        if constexpr (W == 8) {
+            __stcs(reinterpret_cast<uint4*>(p), make_uint4(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3]),
+                                                           pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7])));
+        } else if constexpr (W == 4) {
+            __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])));
+        } else {
+            static_assert(W == 1, "one, four or eight bf16");
+            __stcs(reinterpret_cast<unsigned short*>(p), (unsigned short)(pack2_bf16(x[0], 0.0f) & 0xffffu));
+        }
+    }
+}
+
+// Can rows of `stride` elements of `size` bytes from `base` be read or written W elements at a time?
+inline bool rows_aligned(const void* base, size_t stride, size_t size, int W) {
+    const size_t a = size * (size_t)W < 16 ? size * (size_t)W : 16;
+    return reinterpret_cast<uintptr_t>(base) % a == 0 && stride * size % a == 0;
+}
+
+// f(element type of a, element type of b) for two dtypes that are EC_F32 or EC_BF16.
+template <class F>
+inline auto with_types(ec_dtype_t a, ec_dtype_t b, F f) {
+    if (a == EC_F32) return b == EC_F32 ? f(float{}, float{}) : f(float{}, bf16_t{});
+    return b == EC_F32 ? f(bf16_t{}, float{}) : f(bf16_t{}, bf16_t{});
+}
+inline bool is_real_dtype(ec_dtype_t d) { return d == EC_F32 || d == EC_BF16; }
+
+}  // namespace ec

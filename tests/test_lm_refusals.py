@@ -1,0 +1,47 @@
+"""Arguments the language-model operators refuse on the host, before any launch (no GPU needed)."""
+import ctypes as C
+
+import pytest
+
+
+@pytest.fixture(scope="module")
+def lib():
+    from paper_2203_17063_b200 import binding, build
+
+    build.build()
+    return binding.lib()
+
+
+P = C.c_void_p(4096)                 # stands for a device address: none of these calls gets as far as using it
+INVALID, UNSUPPORTED, CAPACITY = -1, -2, -5
+
+
+def call(fn, good, **change):
+    args = dict(good, **change)
+    return fn(*args.values())
+
+
+def test_embed_lookup(lib):
+    good = dict(table=P, V=8, D=16, table_stride=16, table_dtype=0, tokens=P, index=1, T=4, scale=1.0, out=P, out_stride=16, out_dtype=1, stream=None)
+    for change in (dict(table=None), dict(tokens=None), dict(out=None), dict(V=0), dict(D=0), dict(V=1 << 31), dict(T=1 << 31),
+                   dict(D=(1 << 24) + 1), dict(table_stride=15), dict(out_stride=15), dict(index=2)):
+        assert call(lib.ec_embed_lookup, good, **change) == INVALID, change
+    for change in (dict(table_dtype=2), dict(out_dtype=3), dict(table_dtype=-1)):
+        assert call(lib.ec_embed_lookup, good, **change) == UNSUPPORTED, change
+    assert call(lib.ec_embed_lookup, good, T=0, tokens=None, out=None) == 0
+
+
+def test_embed_grad(lib):
+    need = lib.ec_embed_grad_workspace_bytes(4, 8, 16)
+    assert need > 0 and need % 256 == 0
+    assert lib.ec_embed_grad_workspace_bytes(4, 0, 16) == 0 and lib.ec_embed_grad_workspace_bytes(4, 8, 0) == 0
+    assert lib.ec_embed_grad_workspace_bytes(1 << 30, 1 << 30, 16) == 0
+    good = dict(dout=P, dout_stride=16, dout_dtype=0, tokens=P, index=0, T=4, V=8, D=16, scale=1.0, skip=-1, accumulate=0, grad=P,
+                grad_stride=16, grad_dtype=0, workspace=P, workspace_bytes=need, stream=None)
+    for change in (dict(dout=None), dict(tokens=None), dict(grad=None), dict(V=0), dict(D=0), dict(T=1 << 31), dict(dout_stride=15),
+                   dict(grad_stride=15), dict(index=-1), dict(T=1 << 30, V=1 << 30)):
+        assert call(lib.ec_embed_grad, good, **change) == INVALID, change
+    for change in (dict(dout_dtype=2), dict(grad_dtype=3)):
+        assert call(lib.ec_embed_grad, good, **change) == UNSUPPORTED, change
+    for change in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=C.c_void_p(4096 + 16))):
+        assert call(lib.ec_embed_grad, good, **change) == CAPACITY, change
