@@ -548,6 +548,40 @@ int ec_embed_grad(const void* dout, size_t dout_stride, ec_dtype_t dout_dtype, c
                   size_t V, size_t D, float scale, int64_t skip_token, int accumulate, void* grad, size_t grad_stride,
                   ec_dtype_t grad_dtype, void* workspace, size_t workspace_bytes, ec_stream_t stream);
 
+/* Distillation from a teacher's top logits.  For every token t, a row of student logits z [V] and a list of K teacher
+ * entries (column i_k, teacher logit l_k):
+ *   u = z / temperature,  lse = log sum_v exp(u_v),  a_k = l_k / temperature
+ *   p_k = exp(a_k - teacher_lse[t]), or with teacher_lse == NULL the softmax of a over the row's own entries
+ *   loss[t] = weight[t] * sum_k p_k (log p_k - u_{i_k} + lse)          (0 where p_k = 0)
+ *   grad[t][v] = weight[t] dloss[t] / temperature * (m exp(u_v - lse) - sum over k with i_k = v of p_k),   m = sum_k p_k
+ * i.e. the Kullback-Leibler divergence from the teacher's listed distribution, and its gradient by z.
+ *
+ *   logits      device [T][V], rows logits_stride apart, any alignment of the element type (rows on 16-byte boundaries
+ *               are not needed for the vector path)
+ *   top_index   device int32 or int64 [T][K]; an entry outside [0, V) - -1 pads short lists - is absent; an index listed
+ *               twice counts twice
+ *   top_logit   device fp32 or bf16 [T][K]; -inf: p_k = 0
+ *   weight      device fp32 [T] or NULL (ones).  A row with weight 0, without an entry (or, without teacher_lse, with
+ *               entries of -inf only), or with logits of -inf only is skipped: loss 0, lse -inf, gradient 0, whatever its
+ *               other values are.  Columns of -inf (a padded vocabulary) get gradient 0.
+ *   loss, lse   device fp32 [T], written;  ec_distill_grad reads lse as ec_distill_loss left it
+ *   dloss       device fp32 [T] or NULL (ones): gradient of what follows by loss[t]; 0 skips the row
+ *   grad        device [T][V] of the logits' type, rows grad_stride apart; may be the logits themselves (same stride)
+ * ec_distill_loss reads the logits once; ec_distill_grad reads them once and writes the gradient; ec_distill_step is both
+ * with dloss = 1 while reading the logits once.  Limits: 1 <= V < 2^31 - 1, T < 2^31 - 1, 1 <= K <= EC_DISTILL_MAX_TOP
+ * (EC_ERR_CAPACITY above), 0 < temperature < inf.  One launch each. */
+#define EC_DISTILL_MAX_TOP 256
+int ec_distill_loss(const void* logits, size_t logits_stride, ec_dtype_t dtype, size_t T, size_t V, const void* top_index,
+                    ec_index_t index, const void* top_logit, ec_dtype_t top_dtype, int K, float temperature, const float* weight,
+                    const float* teacher_lse, float* loss, float* lse, ec_stream_t stream);
+int ec_distill_grad(const void* logits, size_t logits_stride, ec_dtype_t dtype, size_t T, size_t V, const void* top_index,
+                    ec_index_t index, const void* top_logit, ec_dtype_t top_dtype, int K, float temperature, const float* weight,
+                    const float* teacher_lse, const float* lse, const float* dloss, void* grad, size_t grad_stride,
+                    ec_stream_t stream);
+int ec_distill_step(const void* logits, size_t logits_stride, ec_dtype_t dtype, size_t T, size_t V, const void* top_index,
+                    ec_index_t index, const void* top_logit, ec_dtype_t top_dtype, int K, float temperature, const float* weight,
+                    const float* teacher_lse, float* loss, float* lse, void* grad, size_t grad_stride, ec_stream_t stream);
+
 /* ------------------------------------------------------------------------- */
 const char* ec_strerror(int code);
 /* The cudaError_t of the last failed CUDA call on this thread (0 if none). */

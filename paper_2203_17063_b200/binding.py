@@ -18,6 +18,7 @@ F32, BF16, I64, F64 = 0, 1, 2, 3
 SUM, MAX, MIN = 0, 1, 2
 ORDER_FIXED, ORDER_PAIRWISE, ORDER_RING = 0, 1, 2
 MAX_RANKS = 1024
+DISTILL_MAX_TOP = 256
 
 OK, ERR_INVALID, ERR_UNSUPPORTED, ERR_CUDA, ERR_STATE, ERR_CAPACITY = 0, -1, -2, -3, -4, -5
 
@@ -67,6 +68,9 @@ SYMBOLS = {
     "ec_embed_lookup": (_i, [_vp, _sz, _sz, _sz, _i, _vp, _i, _sz, C.c_float, _vp, _sz, _i, _vp]),
     "ec_embed_grad_workspace_bytes": (_sz, [_sz, _sz, _sz]),
     "ec_embed_grad": (_i, [_vp, _sz, _i, _vp, _i, _sz, _sz, _sz, C.c_float, C.c_int64, _i, _vp, _sz, _i, _vp, _sz, _vp]),
+    "ec_distill_loss": (_i, [_vp, _sz, _i, _sz, _sz, _vp, _i, _vp, _i, _i, C.c_float, _vp, _vp, _vp, _vp, _vp]),
+    "ec_distill_grad": (_i, [_vp, _sz, _i, _sz, _sz, _vp, _i, _vp, _i, _i, C.c_float, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "ec_distill_step": (_i, [_vp, _sz, _i, _sz, _sz, _vp, _i, _vp, _i, _i, C.c_float, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "ec_strerror": (C.c_char_p, [_i]),
     "ec_last_cuda_error": (_i, []),
     "ec_version": (_i, []),
@@ -421,3 +425,58 @@ def embed_grad(dout, tokens, grad, workspace, scale: float = 1.0, skip_token: in
     _check(lib().ec_embed_grad(dout.data_ptr(), ds, dd, tokens.data_ptr(), idx, T, V, D, scale, skip_token,
                                1 if accumulate else 0, grad.data_ptr(), gs, gd, workspace.data_ptr(), workspace.numel(),
                                _stream(stream)), "ec_embed_grad")
+
+
+def _row_floats(t, T: int, what: str):
+    """Device pointer of an fp32 tensor of T elements (None: NULL)."""
+    if t is None:
+        return None
+    if t.dtype != torch.float32:
+        raise EcError(ERR_UNSUPPORTED, f"{what}: fp32 expected")
+    if t.numel() != T or not t.is_cuda or not t.is_contiguous():
+        raise EcError(ERR_INVALID, f"{what}: one contiguous device value per row expected")
+    return t.data_ptr()
+
+
+def _distill_args(what, logits, top_index, top_logit, temperature, weight, teacher_lse):
+    T, V, stride, dtype = _rows(logits, what + " logits")
+    _, K, ls, top_dtype = _rows(top_logit, what + " top_logit")
+    index = _ids(top_index, what + " top_index")
+    if top_index.shape != top_logit.shape or top_logit.shape[0] != T or (T > 1 and ls != K):
+        raise EcError(ERR_INVALID, f"{what}: top_index and top_logit must be contiguous, [rows of logits][K]")
+    return (logits.data_ptr(), stride, dtype, T, V, top_index.data_ptr(), index, top_logit.data_ptr(), top_dtype, K, temperature,
+            _row_floats(weight, T, what + " weight"), _row_floats(teacher_lse, T, what + " teacher_lse"))
+
+
+def _distill_out(what, logits, grad):
+    T, V, stride, dtype = _rows(grad, what + " grad")
+    if grad.shape != logits.shape or grad.dtype != logits.dtype:
+        raise EcError(ERR_INVALID, f"{what}: grad must have the shape and type of logits")
+    return grad.data_ptr(), stride
+
+
+def distill_loss(logits, top_index, top_logit, loss, lse, temperature: float = 1.0, weight=None, teacher_lse=None,
+                 stream=None) -> None:
+    """ec_distill_loss: per-token divergence from the teacher's listed entries; lse is kept for distill_grad."""
+    args = _distill_args("distill_loss", logits, top_index, top_logit, temperature, weight, teacher_lse)
+    T = args[3]
+    _check(lib().ec_distill_loss(*args, _row_floats(loss, T, "distill_loss loss"), _row_floats(lse, T, "distill_loss lse"),
+                                 _stream(stream)), "ec_distill_loss")
+
+
+def distill_grad(logits, top_index, top_logit, lse, grad, temperature: float = 1.0, weight=None, teacher_lse=None, dloss=None,
+                 stream=None) -> None:
+    """ec_distill_grad: gradient by the logits (grad may be logits itself), given lse of distill_loss."""
+    args = _distill_args("distill_grad", logits, top_index, top_logit, temperature, weight, teacher_lse)
+    T = args[3]
+    _check(lib().ec_distill_grad(*args, _row_floats(lse, T, "distill_grad lse"), _row_floats(dloss, T, "distill_grad dloss"),
+                                 *_distill_out("distill_grad", logits, grad), _stream(stream)), "ec_distill_grad")
+
+
+def distill_step(logits, top_index, top_logit, loss, lse, grad, temperature: float = 1.0, weight=None, teacher_lse=None,
+                 stream=None) -> None:
+    """ec_distill_step: loss and gradient (of the sum of loss) in one pass over the logits."""
+    args = _distill_args("distill_step", logits, top_index, top_logit, temperature, weight, teacher_lse)
+    T = args[3]
+    _check(lib().ec_distill_step(*args, _row_floats(loss, T, "distill_step loss"), _row_floats(lse, T, "distill_step lse"),
+                                 *_distill_out("distill_step", logits, grad), _stream(stream)), "ec_distill_step")

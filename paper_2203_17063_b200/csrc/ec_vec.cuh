@@ -54,6 +54,12 @@ __device__ __forceinline__ void unpack(const raw_vec<T, W>& r, float (&x)[W]) {
 template <class T, int W>
 __device__ __forceinline__ void load_vec(const T* p, float (&x)[W]) { unpack<T, W>(load_raw<T, W>(p), x); }
 
+template <class T>
+__device__ __forceinline__ float unpack_one(T v) {
+    if constexpr (sizeof(T) == 4) return v;
+    else return __uint_as_float((uint32_t)v.bits << 16);
+}
+
 template <class T, int W>
 __device__ __forceinline__ void store_vec(T* p, const float (&x)[W]) {   // written once: not kept in L1
     if constexpr (sizeof(T) == 4) {

@@ -1,0 +1,290 @@
+"""Distillation from a teacher's top logits against the formulas in 64 bits.
+
+Tolerances (u = 2^-24).  The exponent of exp(u_v - lse) is off by at most 4 u (|u_v| + |lse| + 1): the rounded factor
+log2(e) / temperature (2 u relative), the subtracted term and the difference (u each); ex2 itself by 4 u; the sum of V
+exponentials by (V / 256 + 64) u whatever its split over threads.  e_q is their sum; e_p the same for the teacher's entries
+(sum of at most 256).  gradient: |g| (m q e_q + (m q + p) e_p) + 4 u |gradient|; loss: w sum p (|log p| + |u| + |lse| + 1) (e_p +
+4 u), as every logarithm in it is off by less than e_q or e_p times 1 + its size.  Rounding is monotone, so an output lies
+between round(exact - e) and round(exact + e) in its own type."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2203_17063_b200 import binding as ec
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+U = 2.0 ** -24
+
+
+def rows(T, V, dtype, pad, offset, fill=float("nan")):
+    """[T][V] view of a larger allocation filled with `fill`: rows V + pad apart, `offset` elements in."""
+    big = torch.full((offset + T * (V + pad) + 8,), fill, dtype=dtype, device="cuda")
+    return big, big[offset:offset + T * (V + pad)].view(T, V + pad)[:, :V]
+
+
+def problem(T, V, K, seed, idx=torch.int32, top=torch.float32, std=3.0):
+    g = torch.Generator().manual_seed(seed)
+    z = torch.randn(T, V, generator=g, dtype=torch.float64) * std
+    i = torch.randint(0, V, (T, K), generator=g)                          # small vocabularies: repeated entries
+    i[torch.rand(T, K, generator=g) < 0.15] = -1
+    i[torch.rand(T, K, generator=g) < 0.05] = V
+    l = torch.randn(T, K, generator=g, dtype=torch.float64) * 2 + 3
+    w = torch.rand(T, generator=g) + 0.25
+    return z.cuda(), i.to(idx).cuda(), l.to(top).cuda(), w.cuda()
+
+
+def reference(z, i, l, tau, w, teacher_lse, dloss=None, lse=None):
+    """loss, lse, gradient in 64 bits and the bounds of the fp32 forms, by the definitions."""
+    T, V = z.shape
+    z, l, i = z.double(), l.double(), i.long()
+    tau = float(tau)
+    u = z / tau
+    there = (i >= 0) & (i < V)
+    a = torch.where(there, l / tau, torch.full_like(l, -math.inf))
+    A = torch.logsumexp(a, 1) if teacher_lse is None else teacher_lse.double()
+    full = torch.logsumexp(u, 1)
+    L = full if lse is None else lse.double()
+    w = torch.ones(T, dtype=torch.float64, device=z.device) if w is None else w.double()
+    wg = w if dloss is None else w * dloss.double()
+    skip = (wg == 0) | ~there.any(1) | (L == -math.inf)
+    if teacher_lse is None:
+        skip |= A == -math.inf
+    A0 = torch.where(A.isinf(), torch.zeros_like(A), A)
+    logp = a - A0[:, None]
+    p = torch.where(there, logp.exp(), torch.zeros_like(a))
+    logp = torch.where(p > 0, logp, torch.zeros_like(logp))
+    m = p.sum(1)
+    at = i.clamp(0, V - 1)
+    ut = u.gather(1, at)
+    L0 = torch.where(L.isinf(), torch.zeros_like(L), L)
+    term = torch.where(p > 0, p * (logp - ut + L0[:, None]), torch.zeros_like(p))
+    loss = w * term.sum(1)
+    q = (u - L0[:, None]).exp()
+    g = wg / tau
+    pv = torch.zeros_like(u).scatter_add_(1, at, p)
+    grad = g[:, None] * (m[:, None] * q - pv)
+    usize = torch.where(u.isinf(), torch.zeros_like(u), u.abs())
+    e_q = U * (4 * (usize + L0.abs()[:, None] + 1) + 4 + V / 256 + 64)
+    asize = torch.where(a.isinf(), torch.zeros_like(a), a.abs())
+    e_p = U * (4 * (asize.amax(1) + A0.abs() + 1) + 4 + 256)
+    e_grad = g.abs()[:, None] * (m[:, None] * q * e_q + (m[:, None] * q + pv) * e_p[:, None]) + 4 * U * grad.abs()
+    utop = torch.where(ut.isinf(), torch.zeros_like(ut), ut.abs())
+    size = logp.abs() + utop + L0.abs()[:, None] + 1
+    e_loss = w.abs() * (p * size * (e_p[:, None] + 4 * U)).sum(1) + w.abs() * m * U * (V / 256 + 64) + 4 * U * loss.abs()
+    e_lse = U * (V / 256 + 64) + 4 * U * (full.abs() + 1)
+    zero = torch.zeros_like(loss)
+    loss, e_loss = torch.where(skip, zero, loss), torch.where(skip, zero, e_loss)
+    e_lse = torch.where(skip, zero, e_lse)
+    full = torch.where(skip, torch.full_like(full, -math.inf), full)
+    grad = torch.where(skip[:, None], torch.zeros_like(grad), grad)
+    e_grad = torch.where(skip[:, None], torch.zeros_like(e_grad), e_grad)
+    return loss, e_loss, full, e_lse, grad, e_grad
+
+
+def within(got, want, bound, what):
+    low, high = (want - bound).float().to(got.dtype), (want + bound).float().to(got.dtype)
+    ok = ((low <= got) & (got <= high)) | (want.isinf() & (got.double() == want))
+    assert bool(ok.all()), f"{what}: {int((~ok).sum())} values off, first {got[~ok][0].item()} for {want[~ok][0].item()}"
+
+
+def run_all(z, i, l, tau, w, tl, pad=0, offset=0, gpad=None, goffset=None):
+    """The three calls; checks loss, lse and gradients against the reference, and what must not be written."""
+    T, V = z.shape
+    gpad, goffset = pad if gpad is None else gpad, offset if goffset is None else goffset
+    _, zz = rows(T, V, z.dtype, pad, offset)
+    zz.copy_(z)
+    loss, lse = torch.full((T,), 9.0, device="cuda"), torch.full((T,), 9.0, device="cuda")
+    ec.distill_loss(zz, i, l, loss, lse, tau, w, tl)
+    want = reference(z, i, l, tau, w, tl)
+    torch.cuda.synchronize()
+    within(loss, want[0], want[1], "loss")
+    within(lse, want[2], want[3], "lse")
+    big, grad = rows(T, V, z.dtype, gpad, goffset, fill=5.0)
+    step_loss, step_lse = torch.full((T,), 9.0, device="cuda"), torch.full((T,), 9.0, device="cuda")
+    ec.distill_step(zz, i, l, step_loss, step_lse, grad, tau, w, tl)
+    torch.cuda.synchronize()
+    within(step_loss, want[0], want[1], "step's loss")
+    within(step_lse, want[2], want[3], "step's lse")
+    within(grad, want[4], want[5], "step's gradient")
+    outside = torch.ones(big.numel(), dtype=torch.bool, device="cuda")
+    outside[goffset:goffset + T * (V + gpad)].view(T, V + gpad)[:, :V] = False
+    assert bool((big[outside] == 5.0).all()), "written outside the rows"
+    dloss = torch.linspace(-1.0, 2.0, T, device="cuda")
+    dloss[T // 2] = 0.0
+    alone = reference(z, i, l, tau, w, tl, dloss, lse)
+    big, grad2 = rows(T, V, z.dtype, gpad, goffset, fill=5.0)
+    ec.distill_grad(zz, i, l, lse, grad2, tau, w, tl, dloss)
+    torch.cuda.synchronize()
+    within(grad2, alone[4], alone[5], "gradient")
+    assert bool((big[outside] == 5.0).all()), "written outside the rows"
+    again = zz.clone() if pad == 0 and offset == 0 else None
+    if again is not None:                                                  # in place, same bits
+        ec.distill_step(again, i, l, step_loss, step_lse, again, tau, w, tl)
+        torch.cuda.synchronize()
+        assert torch.equal(again, grad)
+        again = zz.clone()
+        ec.distill_grad(again, i, l, lse, again, tau, w, tl, dloss)
+        torch.cuda.synchronize()
+        assert torch.equal(again, grad2)
+    return loss, lse, grad
+
+
+SHAPES = [(1, 1, 1), (3, 2, 1), (5, 7, 9), (4, 8, 4), (2, 31, 8), (9, 255, 3), (6, 1000, 33), (17, 4096, 64), (3, 4097, 256),
+          (5, 8191, 16), (2, 50021, 50), (150, 2048, 8), (1, 131072, 64), (2, 131077, 64), (300, 513, 1), (1, 300001, 100), (2, 600011, 5)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,K", SHAPES)
+def test_against_formulas(cuda_device, T, V, K, dtype):
+    for n, (tau, absolute, idx, top, pad, offset) in enumerate([
+            (1.0, False, torch.int32, torch.float32, 0, 0), (2.5, True, torch.int64, torch.bfloat16, 3, 1), (0.5, False, torch.int64, torch.float32, 8, 8)]):
+        z, i, l, w = problem(T, V, K, 100 + n, idx, top)
+        tl = None
+        if absolute:
+            a = torch.where((i >= 0) & (i < V), l.double() / tau, torch.tensor(-1e30, dtype=torch.float64, device="cuda"))
+            tl = (torch.logsumexp(a, 1) + 0.3).float()
+        run_all(z.to(DT[dtype]), i, l, tau, w, tl, pad, offset)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_gradient_rows_of_another_alignment(cuda_device, dtype):
+    z, i, l, w = problem(7, 1003, 20, 1)
+    run_all(z.to(DT[dtype]), i, l, 1.0, w, None, pad=1, offset=3, gpad=6, goffset=2)
+    run_all(z.to(DT[dtype]), i, l, 1.0, None, None, pad=5, offset=0, gpad=0, goffset=1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 4099, 70001])
+def test_masked_rows_and_columns(cuda_device, V, dtype):
+    T, K = 12, 6
+    z, i, l, w = problem(T, V, K, 2)
+    i = torch.where((i < 0) | (i >= V), torch.zeros_like(i), i)
+    lowest = torch.finfo(DT[dtype]).min
+    z = z.to(DT[dtype])
+    z[0] = -math.inf                                  # no distribution: skipped
+    z[1, V // 2:] = -math.inf                         # a masked half
+    z[2] = -math.inf
+    z[2, V - 1] = 1.0                                 # one column left ...
+    i[2] = V - 1                                      # ... and it is the teacher's
+    z[3, 1:] = lowest                                 # masked with the type's lowest value
+    i[3] = 0
+    z[5] = float("nan")
+    w[5] = 0.0                                        # weight 0: whatever the row holds
+    i[6] = -1                                         # no entry
+    z[6, 3] = float("nan")
+    l[7] = -math.inf                                  # entries without weight
+    l[8, 1:] = -math.inf                              # one with all of it
+    z[9] += 1000.0                                    # far from zero
+    z[10] -= 1000.0
+    z[11] *= 0.0
+    loss, lse, grad = run_all(z, i, l, 1.0, w, None)
+    for r in (0, 5, 6, 7):
+        assert loss[r].item() == 0.0 and lse[r].item() == -math.inf and not grad[r].any()
+    assert not grad[1, V // 2:][~torch.isin(torch.arange(V // 2, V, device="cuda"), i[1])].any()
+    assert abs(grad[2, V - 1].item()) < 1e-5            # q = 1 there, and the six entries (one column) add up to 1
+
+
+def test_rows_of_the_lowest_value_are_uniform(cuda_device):
+    """A row masked throughout with the type's lowest value is a uniform distribution, not a NaN."""
+    V = 1024
+    for dtype in (torch.float32, torch.bfloat16):
+        z = torch.full((2, V), torch.finfo(dtype).min, dtype=dtype, device="cuda")
+        z[1] = torch.finfo(dtype).max
+        i, l = torch.zeros(2, 1, dtype=torch.int32, device="cuda"), torch.ones(2, 1, device="cuda")
+        loss, lse, grad = torch.empty(2, device="cuda"), torch.empty(2, device="cuda"), torch.empty_like(z)
+        ec.distill_step(z, i, l, loss, lse, grad)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(grad).all()) and bool(torch.isfinite(loss).all())
+        assert bool((grad[:, 1:] == 2.0 ** -10).all())
+        ec.distill_grad(z, i, l, lse, grad)
+        torch.cuda.synchronize()
+        assert bool(torch.isfinite(grad).all())
+
+
+def test_masked_teacher_entry_gives_infinite_loss(cuda_device):
+    z = torch.zeros(1, 16, device="cuda")
+    z[0, 4] = -math.inf
+    i, l = torch.tensor([[3, 4]], dtype=torch.int32, device="cuda"), torch.zeros(1, 2, device="cuda")
+    loss, lse, grad = torch.empty(1, device="cuda"), torch.empty(1, device="cuda"), torch.empty_like(z)
+    ec.distill_step(z, i, l, loss, lse, grad)
+    torch.cuda.synchronize()
+    assert loss.item() == math.inf and grad[0, 4].item() == -0.5 and bool(torch.isfinite(grad).all())
+
+
+def test_nan_stays_visible(cuda_device):
+    z, i, l, w = problem(2, 5000, 4, 3)
+    i = torch.where((i < 0) | (i >= 5000), torch.zeros_like(i), i)
+    z = z.float()
+    z[0, 4321] = float("nan")
+    loss, lse, grad = torch.empty(2, device="cuda"), torch.empty(2, device="cuda"), torch.empty_like(z)
+    ec.distill_step(z, i, l, loss, lse, grad, 1.0, w)
+    torch.cuda.synchronize()
+    assert loss[0].isnan() and lse[0].isnan() and bool(grad[0].isnan().all()) and bool(torch.isfinite(grad[1]).all())
+
+
+def test_gradient_against_differences(cuda_device):
+    """Central differences of the loss itself.  The loss's third derivative by one u is below p(1-p) < 1/4 times m = 1, so the
+    differences are off by h^2/24 / tau^3, and by the loss's rounding, 2^-20 over 2h."""
+    T, V, K, tau, h = 3, 11, 4, 2.0, 2.0 ** -5
+    z, i, l, _ = problem(T, V, K, 4, std=1.0)
+    z = z.float()
+    loss, lse, grad = torch.empty(T, device="cuda"), torch.empty(T, device="cuda"), torch.empty_like(z)
+    ec.distill_step(z, i, l, loss, lse, grad, tau)
+    up, down = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    for v in range(V):
+        e = torch.zeros_like(z)
+        e[:, v] = h
+        ec.distill_loss(z + e, i, l, up, lse, tau)
+        ec.distill_loss(z - e, i, l, down, lse, tau)
+        torch.cuda.synchronize()
+        diff = (up.double() - down.double()) / (2 * h)
+        assert bool(((diff - grad[:, v].double()).abs() <= h * h / 24 / tau ** 3 + 2.0 ** -20 / (2 * h)).all())
+
+
+def test_step_repeats_bit_for_bit_on_another_stream(cuda_device):
+    z, i, l, w = problem(200, 9001, 32, 5)
+    z = z.to(torch.bfloat16)
+    outs = []
+    streams = [torch.cuda.Stream(), torch.cuda.Stream(), None]
+    torch.cuda.synchronize()
+    for st in streams:
+        loss, lse, grad = torch.empty(200, device="cuda"), torch.empty(200, device="cuda"), torch.empty_like(z)
+        torch.cuda.synchronize()
+        ec.distill_step(z, i, l, loss, lse, grad, 1.5, w, stream=st)
+        outs.append((loss, lse, grad))
+    torch.cuda.synchronize()
+    for o in outs[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(outs[0], o))
+
+
+def test_empty_batch(cuda_device):
+    z = torch.empty(0, 64, device="cuda")
+    i, l = torch.empty(0, 4, dtype=torch.int32, device="cuda"), torch.empty(0, 4, device="cuda")
+    none = torch.empty(0, device="cuda")
+    ec.distill_step(z, i, l, none, none, torch.empty_like(z))
+
+
+def test_binding_refuses(cuda_device):
+    z, i, l = torch.zeros(4, 32, device="cuda"), torch.zeros(4, 3, dtype=torch.int32, device="cuda"), torch.zeros(4, 3, device="cuda")
+    loss, lse, grad = torch.zeros(4, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, 32, device="cuda")
+    many = torch.zeros(4, ec.DISTILL_MAX_TOP + 1, device="cuda")
+    bad = [
+        (lambda: ec.distill_step(z.half(), i, l, loss, lse, grad), ec.ERR_UNSUPPORTED),
+        (lambda: ec.distill_step(z, i.float(), l, loss, lse, grad), ec.ERR_UNSUPPORTED),
+        (lambda: ec.distill_step(z, i[:3], l, loss, lse, grad), ec.ERR_INVALID),
+        (lambda: ec.distill_step(z, i, l[:, :2], loss, lse, grad), ec.ERR_INVALID),
+        (lambda: ec.distill_step(z, i, l, loss[:3], lse, grad), ec.ERR_INVALID),
+        (lambda: ec.distill_step(z, i, l, loss.double(), lse, grad), ec.ERR_UNSUPPORTED),
+        (lambda: ec.distill_step(z, i, l, loss, lse, grad.bfloat16()), ec.ERR_INVALID),
+        (lambda: ec.distill_step(z, i, l, loss, lse, grad, temperature=0.0), ec.ERR_INVALID),
+        (lambda: ec.distill_step(z, i, l, loss, lse, grad, temperature=float("nan")), ec.ERR_INVALID),
+        (lambda: ec.distill_step(z.cpu(), i, l, loss, lse, grad), ec.ERR_INVALID),
+        (lambda: ec.distill_loss(z, many.int(), many, loss, lse), ec.ERR_CAPACITY),
+    ]
+    for call, code in bad:
+        with pytest.raises(ec.EcError) as err:
+            call()
+        assert err.value.code == code

@@ -45,3 +45,24 @@ def test_embed_grad(lib):
         assert call(lib.ec_embed_grad, good, **change) == UNSUPPORTED, change
     for change in (dict(workspace=None), dict(workspace_bytes=need - 1), dict(workspace=C.c_void_p(4096 + 16))):
         assert call(lib.ec_embed_grad, good, **change) == CAPACITY, change
+
+
+def test_distill(lib):
+    inf = float("inf")
+    head = dict(logits=P, stride=64, dtype=1, T=4, V=64, index_ptr=P, index=0, top=P, top_dtype=0, K=8, tau=1.0, weight=None, teacher_lse=None)
+    loss = dict(head, loss=P, lse=P, stream=None)
+    grad = dict(head, lse=P, dloss=None, grad=C.c_void_p(8192), grad_stride=64, s=None)
+    step = dict(head, loss=P, lse=P, grad=C.c_void_p(8192), grad_stride=64, s=None)
+    for fn, good in ((lib.ec_distill_loss, loss), (lib.ec_distill_grad, grad), (lib.ec_distill_step, step)):
+        for change in (dict(logits=None), dict(stride=63), dict(V=0), dict(V=1 << 31), dict(T=1 << 31), dict(index_ptr=None), dict(index=3),
+                       dict(top=None), dict(K=0), dict(K=-1), dict(tau=0.0), dict(tau=-1.0), dict(tau=inf), dict(tau=float("nan")), dict(lse=None)):
+            assert call(fn, good, **change) == INVALID, change
+        for change in (dict(dtype=2), dict(top_dtype=3)):
+            assert call(fn, good, **change) == UNSUPPORTED, change
+        assert call(fn, good, K=257) == CAPACITY
+        assert call(fn, good, T=0, logits=None) == 0
+        if "grad" in good:
+            assert call(fn, good, grad=None) == INVALID and call(fn, good, grad_stride=63) == INVALID
+            assert call(fn, good, grad=P, grad_stride=65) == INVALID                      # in place wants one stride
+        if "loss" in good:
+            assert call(fn, good, loss=None) == INVALID
