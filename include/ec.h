@@ -582,6 +582,27 @@ int ec_distill_step(const void* logits, size_t logits_stride, ec_dtype_t dtype, 
                     ec_index_t index, const void* top_logit, ec_dtype_t top_dtype, int K, float temperature, const float* weight,
                     const float* teacher_lse, float* loss, float* lse, void* grad, size_t grad_stride, ec_stream_t stream);
 
+/* Matrix products grouped by expert.  Rows (tokens) lie sorted by expert: expert e owns the rows displs[e] .. displs[e+1]-1
+ * of x [T][K] and y [T][N], any number of them, none included; w [E][N][K] is contiguous.
+ *   ec_expert_forward       y[r] = W_e x[r]
+ *   ec_expert_input_grad    dx[r] = W_e^T dy[r]
+ *   ec_expert_weight_grad   dW_e = sum over the rows r of e of dy[r] x[r]^T; accumulate nonzero: added to dw.  An expert
+ *                           without rows gets zeros (accumulate: is left as it is)
+ *   displs    device int64 [E+1], ascending within [0, T] - e.g. as ec_allgatherv writes it, so that rows gathered from the
+ *             ranks can be used where they lie.  Rows outside [displs[0], displs[E]) are neither read nor written.
+ *   status    device uint32 or NULL: 0 = done; 1 = displs does not ascend within [0, T], nothing else was written
+ *   dtype     of x, dy and w: EC_BF16 (tensor cores where rows, weights and outputs start on 16-byte boundaries and N and K
+ *             are multiples of 8; fp32 accumulation) or EC_F32 (fp32 units); outputs EC_BF16 or EC_F32
+ * Limits: 1 <= E <= EC_MAX_EXPERTS, 1 <= N, K <= 2^20 (EC_ERR_CAPACITY above), T < 2^31 - 1024.  One launch each. */
+#define EC_MAX_EXPERTS 1024
+int ec_expert_forward(const void* x, size_t x_stride, const int64_t* displs, int E, const void* w, ec_dtype_t dtype, size_t T, int N,
+                      int K, void* y, size_t y_stride, ec_dtype_t y_dtype, uint32_t* status, ec_stream_t stream);
+int ec_expert_input_grad(const void* dy, size_t dy_stride, const int64_t* displs, int E, const void* w, ec_dtype_t dtype, size_t T,
+                         int N, int K, void* dx, size_t dx_stride, ec_dtype_t dx_dtype, uint32_t* status, ec_stream_t stream);
+int ec_expert_weight_grad(const void* dy, size_t dy_stride, const void* x, size_t x_stride, const int64_t* displs, int E,
+                          ec_dtype_t dtype, size_t T, int N, int K, void* dw, ec_dtype_t dw_dtype, int accumulate, uint32_t* status,
+                          ec_stream_t stream);
+
 /* ------------------------------------------------------------------------- */
 const char* ec_strerror(int code);
 /* The cudaError_t of the last failed CUDA call on this thread (0 if none). */

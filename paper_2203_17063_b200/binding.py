@@ -19,6 +19,7 @@ SUM, MAX, MIN = 0, 1, 2
 ORDER_FIXED, ORDER_PAIRWISE, ORDER_RING = 0, 1, 2
 MAX_RANKS = 1024
 DISTILL_MAX_TOP = 256
+MAX_EXPERTS = 1024
 
 OK, ERR_INVALID, ERR_UNSUPPORTED, ERR_CUDA, ERR_STATE, ERR_CAPACITY = 0, -1, -2, -3, -4, -5
 
@@ -71,6 +72,9 @@ SYMBOLS = {
     "ec_distill_loss": (_i, [_vp, _sz, _i, _sz, _sz, _vp, _i, _vp, _i, _i, C.c_float, _vp, _vp, _vp, _vp, _vp]),
     "ec_distill_grad": (_i, [_vp, _sz, _i, _sz, _sz, _vp, _i, _vp, _i, _i, C.c_float, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
     "ec_distill_step": (_i, [_vp, _sz, _i, _sz, _sz, _vp, _i, _vp, _i, _i, C.c_float, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "ec_expert_forward": (_i, [_vp, _sz, _vp, _i, _vp, _i, _sz, _i, _i, _vp, _sz, _i, _vp, _vp]),
+    "ec_expert_input_grad": (_i, [_vp, _sz, _vp, _i, _vp, _i, _sz, _i, _i, _vp, _sz, _i, _vp, _vp]),
+    "ec_expert_weight_grad": (_i, [_vp, _sz, _vp, _sz, _vp, _i, _i, _sz, _i, _i, _vp, _i, _i, _vp, _vp]),
     "ec_strerror": (C.c_char_p, [_i]),
     "ec_last_cuda_error": (_i, []),
     "ec_version": (_i, []),
@@ -480,3 +484,54 @@ def distill_step(logits, top_index, top_logit, loss, lse, grad, temperature: flo
     T = args[3]
     _check(lib().ec_distill_step(*args, _row_floats(loss, T, "distill_step loss"), _row_floats(lse, T, "distill_step lse"),
                                  *_distill_out("distill_step", logits, grad), _stream(stream)), "ec_distill_step")
+
+
+def _expert_weights(w, what: str):
+    """(E, N, K, dtype code) of contiguous device weights [E][N][K]."""
+    code = _REAL.get(w.dtype)
+    if code is None:
+        raise EcError(ERR_UNSUPPORTED, f"{what}: fp32 or bf16 expected")
+    if w.dim() != 3 or not w.is_cuda or not w.is_contiguous():
+        raise EcError(ERR_INVALID, f"{what}: contiguous device weights [E][N][K] expected")
+    E, N, K = w.shape
+    return E, N, K, code
+
+
+def _displs(displs, E: int, what: str) -> int:
+    if displs.dtype != torch.int64 or displs.numel() != E + 1 or not displs.is_cuda or not displs.is_contiguous():
+        raise EcError(ERR_INVALID, f"{what}: displs must be a device int64 tensor of E + 1 entries")
+    return displs.data_ptr()
+
+
+def expert_forward(x, displs, w, y, status=None, stream=None) -> None:
+    """ec_expert_forward: y[r] = W_e x[r] for the rows displs[e] .. displs[e+1] of every expert e."""
+    E, N, K, code = _expert_weights(w, "expert_forward w")
+    T, Kx, xs, xd = _rows(x, "expert_forward x")
+    Ty, Ny, ys, yd = _rows(y, "expert_forward y")
+    if Kx != K or Ny != N or Ty != T or xd != code:
+        raise EcError(ERR_INVALID, "expert_forward: x [T][K], w [E][N][K] of one type and y [T][N] expected")
+    _check(lib().ec_expert_forward(x.data_ptr(), xs, _displs(displs, E, "expert_forward"), E, w.data_ptr(), code, T, N, K,
+                                   y.data_ptr(), ys, yd, _ptr(status), _stream(stream)), "ec_expert_forward")
+
+
+def expert_input_grad(dy, displs, w, dx, status=None, stream=None) -> None:
+    """ec_expert_input_grad: dx[r] = W_e^T dy[r]."""
+    E, N, K, code = _expert_weights(w, "expert_input_grad w")
+    T, Ny, ys, yd = _rows(dy, "expert_input_grad dy")
+    Tx, Kx, xs, xd = _rows(dx, "expert_input_grad dx")
+    if Kx != K or Ny != N or Tx != T or yd != code:
+        raise EcError(ERR_INVALID, "expert_input_grad: dy [T][N], w [E][N][K] of one type and dx [T][K] expected")
+    _check(lib().ec_expert_input_grad(dy.data_ptr(), ys, _displs(displs, E, "expert_input_grad"), E, w.data_ptr(), code, T, N, K,
+                                      dx.data_ptr(), xs, xd, _ptr(status), _stream(stream)), "ec_expert_input_grad")
+
+
+def expert_weight_grad(dy, x, displs, dw, accumulate: bool = False, status=None, stream=None) -> None:
+    """ec_expert_weight_grad: dW_e (+)= sum over the rows of e of dy[r] x[r]^T."""
+    E, N, K, wd = _expert_weights(dw, "expert_weight_grad dw")
+    T, Ny, ys, code = _rows(dy, "expert_weight_grad dy")
+    Tx, Kx, xs, xd = _rows(x, "expert_weight_grad x")
+    if Kx != K or Ny != N or Tx != T or xd != code:
+        raise EcError(ERR_INVALID, "expert_weight_grad: dy [T][N] and x [T][K] of one type and dw [E][N][K] expected")
+    _check(lib().ec_expert_weight_grad(dy.data_ptr(), ys, x.data_ptr(), xs, _displs(displs, E, "expert_weight_grad"), E, code, T, N,
+                                       K, dw.data_ptr(), wd, 1 if accumulate else 0, _ptr(status), _stream(stream)),
+           "ec_expert_weight_grad")

@@ -1,0 +1,225 @@
+"""Products grouped by expert against 64-bit products.
+
+Tolerance: products of two bf16 are exact in fp32; each of the L additions of a sum is off by at most one ulp of a partial
+sum (2^-23 of it, whether an adder rounds or truncates), partial sums are at most the sum of magnitudes.  So a sum is off by at
+most e = 1.01 L 2^-23 sum |a b|; an output lies between round(exact - e) and round(exact + e) in its own type."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2203_17063_b200 import binding as ec
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+def rows(T, D, dtype, pad, offset, fill=float("nan")):
+    big = torch.full((offset + max(T, 1) * (D + pad) + 8,), fill, dtype=dtype, device="cuda")
+    return big, big[offset:offset + max(T, 1) * (D + pad)].view(max(T, 1), D + pad)[:T, :D]
+
+
+def fill_random(t, seed, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    t.copy_(torch.randn(t.shape, generator=g, dtype=torch.float64) * std)
+
+
+def within(got, want, bound, what):
+    low, high = (want - bound).float().to(got.dtype), (want + bound).float().to(got.dtype)
+    ok = (low <= got) & (got <= high)
+    assert bool(ok.all()), f"{what}: {int((~ok).sum())} of {ok.numel()} values off, first {got[~ok][0].item()} for {want[~ok][0].item()}"
+
+
+def bound(L, mag):
+    return 1.01 * max(L, 1) * 2.0 ** -23 * mag
+
+
+def check_all(cuts, T, N, K, dtype, out, pad=0, offset=0, seed=0):
+    """The three calls for experts with the given cuts; rows outside the experts' are NaN and must not matter."""
+    E = len(cuts) - 1
+    displs = torch.tensor(cuts, dtype=torch.int64, device="cuda")
+    _, x = rows(T, K, DT[dtype], pad, offset)
+    _, dy = rows(T, N, DT[dtype], pad, offset)
+    lo, hi = cuts[0], cuts[-1]
+    fill_random(x[lo:hi], seed)
+    fill_random(dy[lo:hi], seed + 1)
+    w_all = torch.full((E * N * K + offset,), float("nan"), dtype=DT[dtype], device="cuda")
+    w = w_all[offset:].view(E, N, K)
+    fill_random(w, seed + 2, K ** -0.5)
+    status = torch.full((1,), 77, dtype=torch.int32, device="cuda")
+    y_all, y = rows(T, N, DT[out], pad, offset, fill=5.0)
+    ec.expert_forward(x, displs, w, y, status)
+    dx_all, dx = rows(T, K, DT[out], pad, offset, fill=5.0)
+    ec.expert_input_grad(dy, displs, w, dx, status)
+    dw_all = torch.full((offset + E * N * K + 8,), 5.0, dtype=DT[out], device="cuda")
+    dw = dw_all[offset:offset + E * N * K].view(E, N, K)
+    ec.expert_weight_grad(dy, x, displs, dw, status=status)
+    more = torch.ones_like(dw) * 0.5
+    ec.expert_weight_grad(dy, x, displs, more, accumulate=True)
+    torch.cuda.synchronize()
+    assert status.item() == 0
+    assert bool((y_all[torch.isnan(rows_mask(y_all, y, lo, hi, N, pad, offset))] == 5.0).all()), "forward wrote elsewhere"
+    assert bool((dx_all[torch.isnan(rows_mask(dx_all, dx, lo, hi, K, pad, offset))] == 5.0).all()), "input grad wrote elsewhere"
+    assert bool((dw_all[:offset] == 5.0).all()) and bool((dw_all[offset + E * N * K:] == 5.0).all())
+    for e in range(E):
+        a, b = cuts[e], cuts[e + 1]
+        xe, de, we = x[a:b].double(), dy[a:b].double(), w[e].double()
+        within(y[a:b], xe @ we.T, bound(K, xe.abs() @ we.abs().T), f"forward, expert {e}")
+        within(dx[a:b], de @ we, bound(N, de.abs() @ we.abs()), f"input grad, expert {e}")
+        want, mag = de.T @ xe, bound(b - a, de.abs().T @ xe.abs())
+        within(dw[e], want, mag if b > a else torch.zeros_like(mag), f"weight grad, expert {e}")
+        within(more[e], want + 0.5, (mag + 2.0 ** -23 * (want.abs() + 0.5)) if b > a else torch.zeros_like(mag), f"accumulated, expert {e}")
+    again = torch.empty_like(dw)
+    ec.expert_weight_grad(dy, x, displs, again)
+    torch.cuda.synchronize()
+    if offset == 0:
+        assert torch.equal(again, dw)
+
+
+def rows_mask(big, view, lo, hi, D, pad, offset):
+    """NaN where the call must not have written."""
+    m = torch.full(big.shape, float("nan"), device="cuda")
+    m[offset:offset + max(view.shape[0], 1) * (D + pad)].view(-1, D + pad)[lo:hi, :D] = 0.0
+    return m
+
+
+CASES = [  # cuts, T, N, K
+    ([0, 1], 1, 8, 8),
+    ([0, 0], 0, 8, 16),
+    ([0, 0, 0, 3], 3, 16, 8),
+    ([2, 5, 5, 6], 9, 24, 40),
+    ([0, 64, 64, 128], 128, 64, 64),
+    ([0, 1, 2, 3, 4, 5, 6, 7, 8], 8, 72, 136),
+    ([0, 127, 128, 257], 257, 128, 128),
+    ([0, 130, 130, 131, 400], 400, 264, 200),
+    ([5, 200, 705], 720, 256, 512),
+    ([0, 300, 301, 1000], 1000, 520, 328),
+    ([0, 2000], 2000, 1000, 72),
+    ([0, 33, 66, 99, 132, 165, 198, 231, 264, 297, 330, 363, 396, 429, 462, 495, 528], 528, 96, 1040),
+]
+ODD = [([0, 3, 3, 10], 10, 7, 5), ([1, 70, 140], 150, 65, 33), ([0, 129], 129, 130, 257), ([0, 1], 1, 1, 1), ([0, 90, 91], 91, 12, 100)]
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("cuts,T,N,K", CASES)
+def test_bf16(cuda_device, cuts, T, N, K, out):
+    check_all(cuts, T, N, K, "bf16", out)
+    check_all(cuts, T, N, K, "bf16", out, pad=8, offset=8, seed=10)
+
+
+@pytest.mark.parametrize("out", ["f32", "bf16"])
+@pytest.mark.parametrize("cuts,T,N,K", CASES[:8] + ODD)
+def test_any_alignment_and_fp32(cuda_device, cuts, T, N, K, out):
+    check_all(cuts, T, N, K, "bf16", out, pad=3, offset=1)
+    check_all(cuts, T, N, K, "f32", out, pad=1, offset=0, seed=20)
+
+
+def test_many_experts(cuda_device):
+    """1024 experts, most without rows; prefix sums over several chunks of experts."""
+    g = torch.Generator().manual_seed(3)
+    n = torch.where(torch.rand(1024, generator=g) < 0.7, 0, torch.randint(0, 5, (1024,), generator=g))
+    n[1023] = 140
+    cuts = [0] + torch.cumsum(n, 0).tolist()
+    check_all(cuts, cuts[-1] + 3, 16, 24, "bf16", "f32")
+
+
+def test_neighbours_of_nan_rows(cuda_device):
+    """One expert's rows are NaN or inf: the others' products do not see them, whatever tile they share."""
+    for N, K in ((64, 72), (256, 136), (13, 9)):
+        cuts = [0, 37, 50, 191, 193, 300]
+        x = torch.randn(300, K, device="cuda").bfloat16()
+        dy = torch.randn(300, N, device="cuda").bfloat16()
+        w = torch.randn(5, N, K, device="cuda").bfloat16()
+        displs = torch.tensor(cuts, device="cuda")
+        def run():
+            y, dx, dw = torch.empty(300, N, device="cuda"), torch.empty(300, K, device="cuda"), torch.empty(5, N, K, device="cuda")
+            ec.expert_forward(x, displs, w, y)
+            ec.expert_input_grad(dy, displs, w, dx)
+            ec.expert_weight_grad(dy, x, displs, dw)
+            torch.cuda.synchronize()
+            return y, dx, dw
+        clean = run()
+        for bad in (1, 3):
+            x[cuts[bad]:cuts[bad + 1]] = float("nan")
+            dy[cuts[bad]:cuts[bad + 1]] = float("inf")
+            w[bad] = float("nan")
+        dirty = run()
+        for e in (0, 2, 4):
+            a, b = cuts[e], cuts[e + 1]
+            assert torch.equal(clean[0][a:b], dirty[0][a:b]) and torch.equal(clean[1][a:b], dirty[1][a:b]) and torch.equal(clean[2][e], dirty[2][e])
+
+
+@pytest.mark.parametrize("cuts", [[0, 10, 5, 20], [-1, 5, 10, 20], [0, 5, 10, 41], [3, 2, 2, 2]])
+def test_bad_displs(cuda_device, cuts):
+    """displs that does not ascend within [0, T]: status 1 and nothing written."""
+    displs = torch.tensor(cuts, dtype=torch.int64, device="cuda")
+    for N, K in ((32, 64), (5, 7)):
+        x, dy = torch.ones(40, K, device="cuda").bfloat16(), torch.ones(40, N, device="cuda").bfloat16()
+        w = torch.ones(3, N, K, device="cuda").bfloat16()
+        y, dx, dw = torch.full((40, N), 5.0, device="cuda"), torch.full((40, K), 5.0, device="cuda"), torch.full((3, N, K), 5.0, device="cuda")
+        status = torch.zeros(3, dtype=torch.int32, device="cuda")
+        ec.expert_forward(x, displs, w, y, status[0:])
+        ec.expert_input_grad(dy, displs, w, dx, status[1:])
+        ec.expert_weight_grad(dy, x, displs, dw, status=status[2:])
+        torch.cuda.synchronize()
+        assert status.tolist() == [1, 1, 1]
+        assert bool((y == 5).all()) and bool((dx == 5).all()) and bool((dw == 5).all())
+
+
+def test_gradients_are_the_derivatives(cuda_device):
+    """f(x, w) = <forward(x, w), dy> is linear in x and in w: differences equal <delta, gradient>, exactly for small integers."""
+    g = torch.Generator().manual_seed(9)
+    cuts, N, K = [0, 40, 40, 171], 48, 64
+    ints = lambda *s: torch.randint(-2, 3, s, generator=g).float().cuda().bfloat16()    # noqa: E731
+    x, dx_, w, dw_, dy = ints(171, K), ints(171, K), ints(3, N, K), ints(3, N, K), ints(171, N)
+    displs = torch.tensor(cuts, device="cuda")
+    y = [torch.empty(171, N, device="cuda") for _ in range(3)]
+    ec.expert_forward(x, displs, w, y[0])
+    ec.expert_forward(x + dx_, displs, w, y[1])
+    ec.expert_forward(x, displs, w + dw_, y[2])
+    gx, gw = torch.empty(171, K, device="cuda"), torch.empty(3, N, K, device="cuda")
+    ec.expert_input_grad(dy, displs, w, gx)
+    ec.expert_weight_grad(dy, x, displs, gw)
+    torch.cuda.synchronize()
+    dot = lambda a, b: (a.double() * b.double()).sum().item()                           # noqa: E731
+    assert dot(y[1] - y[0], dy) == dot(dx_, gx)
+    assert dot(y[2] - y[0], dy) == dot(dw_, gw)
+
+
+def test_two_streams(cuda_device):
+    cuts, N, K = [0, 700, 1500, 1501], 512, 384
+    displs = torch.tensor(cuts, device="cuda")
+    w = torch.randn(3, N, K, device="cuda").bfloat16()
+    xs = [torch.randn(1501, K, device="cuda").bfloat16() for _ in range(2)]
+    alone = [torch.empty(1501, N, device="cuda") for _ in range(2)]
+    for x, y in zip(xs, alone):
+        ec.expert_forward(x, displs, w, y)
+    torch.cuda.synchronize()
+    streams, outs = [torch.cuda.Stream() for _ in range(2)], [torch.zeros(1501, N, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for x, y, st in zip(xs, outs, streams):
+            ec.expert_forward(x, displs, w, y, stream=st)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(alone, outs))
+
+
+def test_binding_refuses(cuda_device):
+    x, w, y = torch.zeros(6, 16, device="cuda").bfloat16(), torch.zeros(2, 8, 16, device="cuda").bfloat16(), torch.zeros(6, 8, device="cuda")
+    displs = torch.tensor([0, 2, 6], device="cuda")
+    many = torch.zeros(ec.MAX_EXPERTS + 1, 1, 16, device="cuda").bfloat16()
+    bad = [
+        (lambda: ec.expert_forward(x.half(), displs, w, y), ec.ERR_UNSUPPORTED),
+        (lambda: ec.expert_forward(x, displs, w.float(), y), ec.ERR_INVALID),
+        (lambda: ec.expert_forward(x, displs.int(), w, y), ec.ERR_INVALID),
+        (lambda: ec.expert_forward(x, displs[:2], w, y), ec.ERR_INVALID),
+        (lambda: ec.expert_forward(x[:, :8], displs, w, y), ec.ERR_INVALID),
+        (lambda: ec.expert_forward(x, displs, w, y[:5]), ec.ERR_INVALID),
+        (lambda: ec.expert_forward(x, displs, w.transpose(1, 2), y), ec.ERR_INVALID),
+        (lambda: ec.expert_input_grad(y, displs, w, x), ec.ERR_INVALID),
+        (lambda: ec.expert_weight_grad(y.bfloat16(), x, displs, w[:, :, :8]), ec.ERR_INVALID),
+        (lambda: ec.expert_forward(x, torch.zeros(many.shape[0] + 1, dtype=torch.int64, device="cuda"), many, y[:, :1]), ec.ERR_CAPACITY),
+    ]
+    for call, code in bad:
+        with pytest.raises(ec.EcError) as err:
+            call()
+        assert err.value.code == code

@@ -66,3 +66,23 @@ def test_distill(lib):
             assert call(fn, good, grad=P, grad_stride=65) == INVALID                      # in place wants one stride
         if "loss" in good:
             assert call(fn, good, loss=None) == INVALID
+
+
+def test_experts(lib):
+    fwd = dict(x=P, x_stride=16, displs=P, E=2, w=P, dtype=1, T=6, N=8, K=16, y=P, y_stride=8, y_dtype=0, status=None, stream=None)
+    inp = dict(dy=P, dy_stride=8, displs=P, E=2, w=P, dtype=1, T=6, N=8, K=16, dx=P, dx_stride=16, dx_dtype=0, status=None, stream=None)
+    wgt = dict(dy=P, dy_stride=8, x=P, x_stride=16, displs=P, E=2, dtype=1, T=6, N=8, K=16, dw=P, dw_dtype=0, accumulate=0, status=None, stream=None)
+    for fn, good in ((lib.ec_expert_forward, fwd), (lib.ec_expert_input_grad, inp), (lib.ec_expert_weight_grad, wgt)):
+        for change in (dict(displs=None), dict(E=0), dict(N=0), dict(K=0), dict(K=-8), dict(T=(1 << 31) - 1024)):
+            assert call(fn, good, **change) == INVALID, change
+        for name in ("x", "dy", "w", "y", "dx", "dw"):
+            if name in good:
+                assert call(fn, good, **{name: None}) == INVALID, name
+        for name, low in (("x_stride", 15), ("dy_stride", 7), ("y_stride", 7), ("dx_stride", 15)):
+            if name in good:
+                assert call(fn, good, **{name: low}) == INVALID, name
+        for change in (dict(dtype=2), {k: 3 for k in good if k.endswith("_dtype")}):
+            assert call(fn, good, **change) == UNSUPPORTED, change
+        strides = {k: 1 << 21 for k in good if k.endswith("_stride")}
+        assert call(fn, good, E=1025) == CAPACITY
+        assert call(fn, good, N=(1 << 20) + 1, **strides) == CAPACITY and call(fn, good, K=(1 << 20) + 1, **strides) == CAPACITY
