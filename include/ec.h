@@ -590,7 +590,8 @@ int ec_distill_step(const void* logits, size_t logits_stride, ec_dtype_t dtype, 
  *                           without rows gets zeros (accumulate: is left as it is)
  *   displs    device int64 [E+1], ascending within [0, T] - e.g. as ec_allgatherv writes it, so that rows gathered from the
  *             ranks can be used where they lie.  Rows outside [displs[0], displs[E]) are neither read nor written.
- *   status    device uint32 or NULL: 0 = done; 1 = displs does not ascend within [0, T], nothing else was written
+ *   status    device uint32 or NULL: 0 = done; 1 = displs does not ascend within [0, T], nothing else was written;
+ *             2 = a bounded wait inside the tensor-core kernel gave up (a fault of the device): the results are not valid
  *   dtype     of x, dy and w: EC_BF16 (tensor cores where rows, weights and outputs start on 16-byte boundaries and N and K
  *             are multiples of 8; fp32 accumulation) or EC_F32 (fp32 units); outputs EC_BF16 or EC_F32
  * Limits: 1 <= E <= EC_MAX_EXPERTS, 1 <= N, K <= 2^20 (EC_ERR_CAPACITY above), T < 2^31 - 1024.  One launch each. */

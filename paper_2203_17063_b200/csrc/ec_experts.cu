@@ -7,7 +7,9 @@
 // Rows are sorted by expert: expert e owns rows displs[e] .. displs[e+1]-1 (displs as ec_allgatherv leaves it, on the
 // device: the host never learns the sizes).  Every block derives the list of tiles from displs itself.
 
-#include "ec_vec.cuh"
+#include <atomic>
+
+#include "ec_mma.cuh"
 
 namespace ec {
 namespace {
@@ -160,8 +162,304 @@ __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertA
     }
 }
 
+// ---- products on the tensor cores --------------------------------------------------------------------------------
+// One persistent block per SM, 128 x bn tiles of the result, reduction in steps of 64:
+//   producer (one thread)  brings the two operand tiles of a step into a ring of shared-memory stages by bulk tensor copies.
+//                          Rows of another expert that a copy brings along only reach result rows that are not stored; where
+//                          rows are the reduction (weight grad) the last step's foreign rows are overwritten with zeros
+//                          before the product, both operands, since they may hold infinities or NaN;
+//   issuer (one warp)      multiplies a landed stage, as it lies, into one of two accumulators in tensor memory;
+//   epilogue (four warps)  reads the finished accumulator while the next tile's products run, rounds once and writes it out
+//                          through a small transposing buffer, so that a warp's stores cover whole 128-byte lines.
+// Operands: x and dy are K-major where their columns are the reduction, MN-major in the weight grad; W is K-major in the
+// forward and MN-major in the input grad: no operand is transposed in memory.
+// Every wait is bounded; a wait that gives up raises a flag that all roles poll, the block sets *status to 2, waits for its
+// copies in flight, frees its tensor memory and returns.
+
+constexpr int MM_THREADS = 256, MM_ROWS = 128, MM_STEP = 64, MM_MAX_STAGES = 8;
+constexpr int MM_PITCH = 144;                                  // bytes of a 128-byte row in the transposing buffer
+
+struct MmaPlan {
+    int bm, bn, stages;                                        // rows a tile takes (<= 128), columns, ring stages
+    uint32_t a_bytes, b_bytes, stage_bytes, tx_bytes, tmem_cols, idesc, smem;
+};
+
+// One warp writes its 32 rows (`height` of them exist) of a finished tile, `width` columns from tensor-memory column src on
+// (there: false - no products were made, the tile is zero).  Values are staged as S: as TO, or in fp32 when they are added to
+// what is there, so that the sum is rounded once.
+template <class TO, class S, bool ADD>
+__device__ __forceinline__ void store_tile(TO* out, size_t stride, int height, int width, uint32_t src, bool there, unsigned char* buf, int lane) {
+    constexpr int PER = 128 / (int)sizeof(S), W = 16 / (int)sizeof(S);       // columns of a 128-byte piece of a row, of a lane's part
+    for (int c0 = 0; c0 < width; c0 += PER) {
+#pragma unroll
+        for (int p = 0; p < PER / 32; ++p) {
+            if (p > 0 && c0 + p * 32 >= width) break;
+            uint32_t v[32];
+            if (there) {
+                mma::tmem_ld32(src + (uint32_t)(c0 + p * 32), v);
+                mma::tmem_ld_wait();
+            } else {
+#pragma unroll
+                for (int q = 0; q < 32; ++q) v[q] = 0u;
+            }
+            uint4* row = reinterpret_cast<uint4*>(buf + lane * MM_PITCH + p * 32 * (int)sizeof(S));
+#pragma unroll
+            for (int q = 0; q < 32 / W; ++q) {
+                if constexpr (sizeof(S) == 4) {
+                    row[q] = make_uint4(v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]);
+                } else {
+                    uint32_t h[4];
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) h[r] = pack2_bf16(__uint_as_float(v[8 * q + 2 * r]), __uint_as_float(v[8 * q + 2 * r + 1]));
+                    row[q] = make_uint4(h[0], h[1], h[2], h[3]);
+                }
+            }
+        }
+        __syncwarp();
+        const int c = c0 + (lane & 7) * W;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {                          // eight lanes a row, four rows a step
+            const int r = q * 4 + (lane >> 3);
+            if (r < height && c < width) {
+                const uint4 u = *reinterpret_cast<const uint4*>(buf + r * MM_PITCH + (lane & 7) * 16);
+                TO* d = out + (size_t)r * stride + c;
+                if constexpr (ADD) {
+                    float x[W] = {__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w)}, old[W];
+                    load_vec<TO, W>(d, old);
+#pragma unroll
+                    for (int z = 0; z < W; ++z) x[z] += old[z];
+                    store_vec<TO, W>(d, x);
+                } else {
+                    __stcs(reinterpret_cast<uint4*>(d), u);
+                }
+            }
+        }
+        __syncwarp();
+    }
+}
+
+template <class TO, int MODE>
+__global__ void __launch_bounds__(MM_THREADS, 1)
+expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ExpertArgs a, const MmaPlan pl) {
+    using namespace mma;
+    extern __shared__ unsigned char mm_raw[];
+    __shared__ int s_row[MAX_EXPERTS + 1], s_tile[MAX_EXPERTS + 1], s_warp[MM_THREADS / 32];
+    __shared__ __align__(8) uint64_t s_bar[2 * MM_MAX_STAGES + 4];
+    __shared__ uint32_t s_tmem;
+    __shared__ volatile int s_abort;
+    __shared__ __align__(16) unsigned char s_out[4][32 * MM_PITCH];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    if (!expert_ranges<MM_THREADS>(a, pl.bm, s_row, s_tile, s_warp)) return;
+
+    unsigned char* sm = mm_raw + ((1024u - (smem_u32(mm_raw) & 1023u)) & 1023u);
+    const uint32_t stage0 = smem_u32(sm), bar0 = smem_u32(s_bar);
+    auto B_full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
+    auto B_empty = [&](int s) { return bar0 + 8u * (uint32_t)(MM_MAX_STAGES + s); };
+    auto B_accfull = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MM_MAX_STAGES + b); };
+    auto B_accempty = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MM_MAX_STAGES + 2 + b); };
+    if (tid == 0) {
+        for (int s = 0; s < pl.stages; ++s) { mbar_init(B_full(s), 1); mbar_init(B_empty(s), 1); }
+        for (int b = 0; b < 2; ++b) { mbar_init(B_accfull(b), 1); mbar_init(B_accempty(b), 4); }
+        s_abort = 0;
+        mbar_init_fence();
+    }
+    if (warp == 2) tmem_alloc(smem_u32(&s_tmem), pl.tmem_cols);
+    fence_before_sync();
+    __syncthreads();
+    fence_after_sync();
+    const uint32_t tmem = s_tmem;
+
+    // the tiles: for each expert, down the rows first
+    const int cols = MODE == EX_FORWARD ? a.N : a.K, jt = (cols + pl.bn - 1) / pl.bn;
+    const int wt = (a.N + MM_ROWS - 1) / MM_ROWS;
+    const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * wt * jt : (long long)s_tile[a.E] * jt;
+    struct Tile { int e, i, i_end, j, len; };                  // expert, first result row, end of its rows, first column, reduction length
+    auto tile_of = [&](long long t) {
+        Tile x;
+        if (MODE == EX_WEIGHT) {
+            x.e = (int)(t / ((long long)wt * jt));
+            const int q = (int)(t - (long long)x.e * wt * jt);
+            x.i = (q % wt) * MM_ROWS;
+            x.i_end = a.N;
+            x.j = (q / wt) * pl.bn;
+            x.len = s_row[x.e + 1] - s_row[x.e];
+        } else {
+            x.e = expert_of(s_tile, a.E, (int)(t / jt));
+            const int mt = s_tile[x.e + 1] - s_tile[x.e], q = (int)(t - (long long)s_tile[x.e] * jt);
+            x.i = s_row[x.e] + (q % mt) * pl.bm;
+            x.i_end = x.i + pl.bm < s_row[x.e + 1] ? x.i + pl.bm : s_row[x.e + 1];
+            x.j = (q / mt) * pl.bn;
+            x.len = MODE == EX_FORWARD ? a.K : a.N;
+        }
+        return x;
+    };
+
+    bool ok = true;
+    uint32_t filled = 0;                                       // stages the producer has filled
+    if (warp == 0) {
+        if (lane == 0) {
+            for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+                const Tile x = tile_of(t);
+                for (int l = 0; l < x.len; l += MM_STEP) {
+                    const int s = (int)(filled % (uint32_t)pl.stages);
+                    const uint32_t use = filled / (uint32_t)pl.stages;
+                    if (use > 0 && !wait_or_abort(B_empty(s), (use - 1) & 1u, &s_abort)) { ok = false; break; }
+                    const uint32_t sa = stage0 + (uint32_t)s * pl.stage_bytes, sb = sa + pl.a_bytes;
+                    mbar_expect_tx(B_full(s), pl.tx_bytes);
+                    if (MODE == EX_WEIGHT) {
+                        const int r = s_row[x.e] + l;
+                        for (int q = 0; q < MM_ROWS / 64; ++q) tma_load_2d(sa + q * 8192u, &map_a, x.i + 64 * q, r, B_full(s));
+                        for (int q = 0; q < pl.bn / 64; ++q) tma_load_2d(sb + q * 8192u, &map_b, x.j + 64 * q, r, B_full(s));
+                    } else {
+                        tma_load_2d(sa, &map_a, l, x.i, B_full(s));
+                        if (MODE == EX_FORWARD) tma_load_3d(sb, &map_b, l, x.j, x.e, B_full(s));
+                        else for (int q = 0; q < pl.bn / 64; ++q) tma_load_3d(sb + q * 8192u, &map_b, x.j + 64 * q, l, x.e, B_full(s));
+                    }
+                    ++filled;
+                }
+            }
+            if (s_abort != 0)                                  // copies in flight land before the block may go
+                for (uint32_t f = filled > (uint32_t)pl.stages ? filled - pl.stages : 0; f < filled; ++f)
+                    for (uint32_t it = 0; it < (1u << 12); ++it)
+                        if (mbar_try_wait(B_full((int)(f % (uint32_t)pl.stages)), (f / (uint32_t)pl.stages) & 1u)) break;
+        }
+    } else if (warp == 1) {
+        uint32_t n = 0, acc = 0;                               // stages multiplied, accumulators filled
+        for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            if (x.len == 0) continue;
+            const int buf = (int)(acc & 1u);
+            if (acc >= 2) ok = __all_sync(0xffffffffu, wait_or_abort(B_accempty(buf), ((acc >> 1) - 1) & 1u, &s_abort));   // (the warp goes on, or leaves, together)
+            if (!ok) break;
+            fence_after_sync();
+            for (int l = 0; l < x.len; l += MM_STEP) {
+                const int s = (int)(n % (uint32_t)pl.stages);
+                ok = __all_sync(0xffffffffu, wait_or_abort(B_full(s), (n / (uint32_t)pl.stages) & 1u, &s_abort));
+                if (!ok) break;
+                fence_after_sync();
+                const uint32_t sa = stage0 + (uint32_t)s * pl.stage_bytes, sb = sa + pl.a_bytes;
+                if (MODE == EX_WEIGHT && x.len - l < MM_STEP) {
+                    const int keep = x.len - l, boxes = (MM_ROWS + pl.bn) / 64, items = (MM_STEP - keep) * 8;
+                    for (int q = lane; q < boxes * items; q += 32) {
+                        const int box = q / items, p = q - box * items;
+                        *reinterpret_cast<uint4*>(sm + (size_t)s * pl.stage_bytes + box * 8192 + keep * 128 + p * 16) = make_uint4(0, 0, 0, 0);
+                    }
+                    fence_async_smem();
+                    __syncwarp();
+                }
+                if (lane == 0) {
+#pragma unroll
+                    for (int k = 0; k < MM_STEP / 16; ++k) {
+                        const uint64_t da = operand_desc(sa + k * (MODE == EX_WEIGHT ? 2048u : 32u), MODE == EX_WEIGHT ? 8192u : 16u);
+                        const uint64_t db = operand_desc(sb + k * (MODE == EX_FORWARD ? 32u : 2048u), MODE == EX_FORWARD ? 16u : 8192u);
+                        mma_bf16(tmem + (uint32_t)(buf * pl.bn), da, db, pl.idesc, l > 0 || k > 0 ? 1u : 0u);
+                    }
+                    mma_commit(B_empty(s));
+                    if (l + MM_STEP >= x.len) mma_commit(B_accfull(buf));
+                }
+                __syncwarp();
+                ++n;
+            }
+            ++acc;
+        }
+    } else if (warp >= 4) {
+        const int w = warp - 4;
+        uint32_t acc = 0;
+        for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+            const Tile x = tile_of(t);
+            if (MODE == EX_WEIGHT && x.len == 0 && a.accumulate) continue;
+            const int buf = (int)(acc & 1u);
+            if (x.len > 0) {
+                ok = __all_sync(0xffffffffu, wait_or_abort(B_accfull(buf), (acc >> 1) & 1u, &s_abort));
+                if (!ok) break;
+                fence_after_sync();
+                ++acc;
+            }
+            TO* out = static_cast<TO*>(a.out) + (MODE == EX_WEIGHT ? (size_t)x.e * a.N * a.K : 0) + (size_t)(x.i + w * 32) * (MODE == EX_WEIGHT ? (size_t)a.K : a.out_stride) + x.j;
+            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(buf * pl.bn);
+            const int width = cols - x.j < pl.bn ? cols - x.j : pl.bn, height = x.i_end - x.i - w * 32;
+            const size_t os = MODE == EX_WEIGHT ? (size_t)a.K : a.out_stride;
+            if (MODE == EX_WEIGHT && a.accumulate) store_tile<TO, float, true>(out, os, height, width, src, x.len > 0, s_out[w], lane);
+            else store_tile<TO, TO, false>(out, os, height, width, src, x.len > 0, s_out[w], lane);
+            if (x.len > 0) {
+                fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(B_accempty(buf));
+            }
+        }
+    }
+    fence_before_sync();
+    __syncthreads();
+    if (tid == 0 && s_abort != 0 && a.status != nullptr) *a.status = 2u;
+    if (warp == 2) {
+        fence_after_sync();
+        tmem_dealloc(tmem, pl.tmem_cols);
+    }
+}
+
+// The tensor-core form needs rows, weights and results on 16-byte boundaries (bulk tensor copies, 16-byte stores) and
+// row lengths that are multiples of 8.
+bool mma_shape(const ExpertArgs& a, ec_dtype_t dtype, ec_dtype_t out_dtype, int mode) {
+    if (dtype != EC_BF16 || a.T == 0 || a.N % 8 || a.K % 8) return false;
+    if (mode != EX_WEIGHT && !aligned16(a.w)) return false;
+    if (mode != EX_INPUT && (!aligned16(a.x) || a.x_stride % 8)) return false;
+    if (mode != EX_FORWARD && (!aligned16(a.dy) || a.dy_stride % 8)) return false;
+    if (!aligned16(a.out) || (mode != EX_WEIGHT && a.out_stride % (out_dtype == EC_F32 ? 4 : 8))) return false;
+    return mma::encode_tiled() != nullptr;
+}
+
+MmaPlan mma_plan(const ExpertArgs& a, int mode) {
+    MmaPlan p = {};
+    const int cols = mode == EX_FORWARD ? a.N : a.K;
+    p.bm = MM_ROWS;
+    p.bn = 256;
+    while (p.bn > 64 && p.bn / 2 >= cols) p.bn /= 2;
+    p.a_bytes = MM_ROWS * MM_STEP * 2;
+    p.b_bytes = (uint32_t)p.bn * MM_STEP * 2;
+    p.stage_bytes = p.a_bytes + p.b_bytes;
+    p.tx_bytes = p.stage_bytes;
+    p.stages = (int)((200u * 1024u - 1024u) / p.stage_bytes);
+    if (p.stages > MM_MAX_STAGES) p.stages = MM_MAX_STAGES;
+    p.tmem_cols = (uint32_t)p.bn * 2;
+    p.idesc = mma::instr_desc(MM_ROWS, p.bn, mode == EX_WEIGHT, mode != EX_FORWARD);
+    p.smem = (uint32_t)p.stages * p.stage_bytes + 1024u;
+    return p;
+}
+
+template <class TO, int MODE>
+int launch_mma(const ExpertArgs& a, cudaStream_t st) {
+    const MmaPlan p = mma_plan(a, MODE);
+    CUtensorMap ma, mb;
+    const size_t NK = (size_t)a.N * a.K;
+    bool ok;
+    if (MODE == EX_FORWARD)
+        ok = mma::make_map(&ma, a.x, 2, a.K, a.T, 1, a.x_stride, 0, MM_STEP, (unsigned)p.bm) &&
+             mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, MM_STEP, (unsigned)p.bn);
+    else if (MODE == EX_INPUT)
+        ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, MM_STEP, (unsigned)p.bm) &&
+             mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, 64, MM_STEP);
+    else
+        ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, 64, MM_STEP) &&
+             mma::make_map(&mb, a.x, 2, a.K, a.T, 1, a.x_stride, 0, 64, MM_STEP);
+    if (!ok) return EC_ERR_CUDA;
+    int dev = 0, sms = 0;
+    EC_CUDA(cudaGetDevice(&dev));
+    EC_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    static std::atomic<uint64_t> ready{0};                     // devices on which the shared-memory limit is raised
+    if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1u)) {
+        EC_CUDA(cudaFuncSetAttribute(expert_mma_kernel<TO, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024));
+        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    const size_t jt = ((size_t)(MODE == EX_FORWARD ? a.N : a.K) + p.bn - 1) / p.bn;
+    const size_t most = MODE == EX_WEIGHT ? (size_t)a.E * ((a.N + MM_ROWS - 1) / MM_ROWS) * jt : (a.T / p.bm + a.E) * jt;
+    expert_mma_kernel<TO, MODE><<<(unsigned)(most < (size_t)sms ? most : sms), MM_THREADS, p.smem, st>>>(ma, mb, a, p);
+    EC_CUDA(cudaGetLastError());
+    return EC_OK;
+}
+
 template <int MODE>
 int launch_experts(const ExpertArgs& a, ec_dtype_t dtype, ec_dtype_t out_dtype, cudaStream_t st) {
+    if (mma_shape(a, dtype, out_dtype, MODE)) return out_dtype == EC_F32 ? launch_mma<float, MODE>(a, st) : launch_mma<bf16_t, MODE>(a, st);
     return with_types(dtype, out_dtype, [&](auto ti, auto to) {
         using TI = decltype(ti); using TO = decltype(to);
         expert_scalar_kernel<TI, TO, MODE><<<148 * 4, SC_THREADS, 0, st>>>(a);
