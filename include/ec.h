@@ -568,7 +568,7 @@ int ec_embed_grad(const void* dout, size_t dout_stride, ec_dtype_t dout_dtype, c
  *   dloss       device fp32 [T] or NULL (ones): gradient of what follows by loss[t]; 0 skips the row
  *   grad        device [T][V] of the logits' type, rows grad_stride apart; may be the logits themselves (same stride)
  * ec_distill_loss reads the logits once; ec_distill_grad reads them once and writes the gradient; ec_distill_step is both
- * with dloss = 1 while reading the logits once.  Limits: 1 <= V < 2^31 - 1, T < 2^31 - 1, 1 <= K <= EC_DISTILL_MAX_TOP
+ * with dloss = 1 while reading the logits once.  Limits: 1 <= V < 2^31 - 4096, T < 2^31 - 1, 1 <= K <= EC_DISTILL_MAX_TOP
  * (EC_ERR_CAPACITY above), 0 < temperature < inf.  One launch each. */
 #define EC_DISTILL_MAX_TOP 256
 int ec_distill_loss(const void* logits, size_t logits_stride, ec_dtype_t dtype, size_t T, size_t V, const void* top_index,

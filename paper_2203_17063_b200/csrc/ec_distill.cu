@@ -11,16 +11,15 @@
 // fixed order.  The gradient is first written as if no entry were in the teacher's list; the list's entries follow behind a
 // barrier, each written by the block that owns its column.
 
-#include <cooperative_groups.h>
+#include <atomic>
 
 #include "ec_vec.cuh"
 
 namespace ec {
 namespace {
 
-namespace cg = cooperative_groups;
-
 constexpr int MAX_TOP = EC_DISTILL_MAX_TOP;
+constexpr size_t MAX_V = 0x7fffffffull - 4096;                     // a column past the last part still has a number
 constexpr float LOG2E = 1.44269504088896340736f, LOG2E_REST = 1.92596299112661746887e-8f;   // log2 e = LOG2E + LOG2E_REST
 
 enum { MODE_LOSS = 0, MODE_GRAD = 1, MODE_STEP = 2 };
@@ -51,14 +50,14 @@ __device__ __forceinline__ float warp_sum(float x) {
     for (int d = 16; d > 0; d >>= 1) x += __shfl_xor_sync(0xffffffffu, x, d);
     return x;
 }
-// exp2(c (x - m)) for logits x, m: one fused multiply-add where c m is far inside fp32's range, else (rows masked with the
-// type's lowest value throughout) by the difference, which cannot overflow to a NaN.
-struct Below {
-    float c, m, cm;
-    bool fused;
-    __device__ Below(float c_, float m_) : c(c_), m(m_ == -INFINITY ? 0.0f : m_), cm(c_ * m), fused(fabsf(cm) < 1e38f) {}
-    __device__ float operator()(float x) const { return ex2(fused ? fmaf(x, c, -cm) : (x - m) * c); }
-};
+// a value in the shared memory of block `rank` of the cluster
+__device__ __forceinline__ float2 peer(const float2* p, int rank) {
+    uint32_t addr;
+    float2 x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(addr) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(addr) : "memory");
+    return x;
+}
 // (maximum, sum below it) of two parts; a part without anything has maximum -inf and sum 0
 __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, float c) {
     const float top = fmaxf(m, m2), ref = top == -INFINITY ? 0.0f : top;
@@ -66,59 +65,43 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2, flo
     m = top;
 }
 
-// Rows may start anywhere on the element grid.  A row is seen as vectors of 16 bytes on the 16-byte grid; its first and last
-// vector may stick out of it and are then accessed element by element.
+// Rows may start anywhere on the element grid: a row is its whole 16-byte vectors on the 16-byte grid, and fewer than a vector's
+// elements before and behind them.  A part is a run of consecutive vectors; the first part also has the elements before them, the
+// last part those behind, one element a thread.
 template <class T>
-struct Row {
+struct Part {
     static constexpr int W = 16 / (int)sizeof(T);
-    const T* p;              // first element
-    size_t V;
-    int h;                   // elements between the 16-byte boundary at or before p and p
-    __device__ Row(const T* p_, size_t V_) : p(p_), V(V_), h((int)((reinterpret_cast<uintptr_t>(p_) & 15u) / sizeof(T))) {}
-    __device__ size_t vectors() const { return (V + h + W - 1) / W; }
-    __device__ bool whole(size_t i) const { return i * W >= (size_t)h && (i + 1) * W <= V + h; }
-    __device__ raw_vec<T, W> load(size_t i) const {
-        if (whole(i)) return load_raw<T, W>(p - h + i * W);
-        raw_vec<T, W> r;
-#pragma unroll
-        for (int e = 0; e < W; ++e) {
-            const size_t x = i * W + e;
-            uint32_t b = sizeof(T) == 4 ? 0xff800000u : 0xff80u;          // -inf: nothing there
-            if (x >= (size_t)h && x < V + h) b = load_raw<T, 1>(p + (x - h)).u[0];
-            if (sizeof(T) == 4) r.u[e] = b;
-            else if (e & 1) r.u[e / 2] |= b << 16;
-            else r.u[e / 2] = b;
-        }
-        return r;
+    const T* p;                      // the part's vectors
+    uint32_t n;
+    int col0, col1, col;             // columns [col0, col1) are the part's; column of its first vector
+    int edge;                        // column of this thread's single element, -1: none
+    __device__ Part(const T* row, int V, int part, int parts_log2, int tid) {
+        const int h = (int)(reinterpret_cast<uintptr_t>(row) & 15u) / (int)sizeof(T);
+        const int head = h == 0 ? 0 : W - h < V ? W - h : V;
+        const uint32_t all = (uint32_t)(V - head) / W, per = (all + (1u << parts_log2) - 1) >> parts_log2;
+        const int parts = 1 << parts_log2;
+        const uint32_t v0 = part * per < all ? part * per : all;
+        n = all - v0 < per ? all - v0 : per;
+        col = head + (int)v0 * W;
+        col0 = part == 0 ? 0 : col;
+        col1 = part == parts - 1 ? V : col + (int)n * W;
+        p = row + col;
+        edge = -1;
+        if (tid < W && part == 0 && tid < head) edge = tid;
+        const int back = col + (int)n * W + tid - W;
+        if (tid >= W && tid < 2 * W && part == parts - 1 && back < V) edge = back;
     }
 };
-// the same positions of the gradient's row; `aligned`: its rows lie on the 16-byte grid as the logits' rows do
-template <class T>
-__device__ __forceinline__ void store_row(const Row<T>& row, T* dst, bool aligned, size_t i, const float (&x)[16 / sizeof(T)]) {
-    constexpr int W = Row<T>::W;
-    if (aligned && row.whole(i)) {
-        store_vec<T, W>(dst + (i * W - row.h), x);
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < W; ++e) {
-        const size_t c = i * W + e;
-        if (c >= (size_t)row.h && c < row.V + row.h) {
-            const float one[1] = {x[e]};
-            store_vec<T, 1>(dst + (c - row.h), one);
-        }
-    }
-}
 
 // What the block knows of the row's teacher (shared memory).
-struct Teacher {
+struct __align__(8) Teacher {
     float mass, part;        // sum of p_k; sum over the block's own columns of p_k (log p_k - u_k)
     int any;                 // the row has an entry
 };
 
 // One warp: the teacher's entries of row t.  [c0, c1): the block's columns, whose logits are fetched.
 template <class T>
-__device__ void teacher_row(const DistillArgs& a, size_t t, const T* z, size_t c0, size_t c1, int lane, int* s_idx, float* s_p, float* s_z,
+__device__ void teacher_row(const DistillArgs& a, size_t t, const T* z, int c0, int c1, int lane, int* s_idx, float* s_p, float* s_z,
                             Teacher* out) {
     const size_t base = t * (size_t)a.K;
     float top = -INFINITY;
@@ -132,7 +115,7 @@ __device__ void teacher_row(const DistillArgs& a, size_t t, const T* z, size_t c
                             : static_cast<const float*>(a.top_logit)[base + k]) * a.inv_tau;
         s_idx[k] = there ? (int)i : -1;
         s_p[k] = l;
-        s_z[k] = there && (size_t)i >= c0 && (size_t)i < c1 ? unpack_one<T>(z[i]) : 0.0f;
+        s_z[k] = there && i >= c0 && i < c1 ? unpack_one<T>(z[i]) : 0.0f;
         any |= there ? 1 : 0;
         top = l > top || l != l ? l : top;              // (a NaN stays)
     }
@@ -154,7 +137,7 @@ __device__ void teacher_row(const DistillArgs& a, size_t t, const T* z, size_t c
         const float logp = s_p[k] - A, p = s_idx[k] >= 0 ? expf(logp) : 0.0f;
         s_p[k] = p;
         mass += p;
-        if (p != 0.0f && (size_t)s_idx[k] >= c0 && (size_t)s_idx[k] < c1) part += p * (logp - s_z[k] * a.inv_tau);
+        if (p != 0.0f && s_idx[k] >= c0 && s_idx[k] < c1) part += p * (logp - s_z[k] * a.inv_tau);
     }
     mass = warp_sum(mass);
     part = warp_sum(part);
@@ -166,111 +149,293 @@ __device__ void teacher_row(const DistillArgs& a, size_t t, const T* z, size_t c
     __syncwarp();
 }
 
+
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+
+// Sum of exponentials below m (a finite logit, or 0) of N vectors; four chains of additions.
+template <class T, int N>
+__device__ __forceinline__ float sum_below(const raw_vec<T, 16 / (int)sizeof(T)> (&v)[N], float c, float m) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const float cm = c * m;
+    float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (fabsf(cm) < 1e38f) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            float x[W];
+            unpack<T, W>(v[q], x);
+#pragma unroll
+            for (int e = 0; e < W; ++e) s[e & 3] += ex2(fmaf(x[e], c, -cm));
+        }
+    } else {          // rows masked with the type's lowest value throughout: the difference cannot overflow to a NaN
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            float x[W];
+            unpack<T, W>(v[q], x);
+#pragma unroll
+            for (int e = 0; e < W; ++e) s[e & 3] += ex2((x[e] - m) * c);
+        }
+    }
+    return (s[0] + s[1]) + (s[2] + s[3]);
+}
+// Largest of m and N vectors (NaN passes by: it shows in the sum).  bf16 pairs are compared as they are.
+template <class T, int N>
+__device__ __forceinline__ float max_of(const raw_vec<T, 16 / (int)sizeof(T)> (&v)[N], float m) {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) m = fmaxf(m, __uint_as_float(v[q].u[e]));
+        return m;
+    } else {
+        uint32_t top = v[0].u[0];
+#pragma unroll
+        for (int q = 0; q < N; ++q)
+#pragma unroll
+            for (int e = q == 0 ? 1 : 0; e < 4; ++e) asm("max.bf16x2 %0, %1, %2;" : "=r"(top) : "r"(top), "r"(v[q].u[e]));
+        return fmaxf(m, fmaxf(bf16_lo(top), bf16_hi(top)));
+    }
+}
+// Keeps the compiler from carrying the unpacked values from one pass over the vectors to the next: packed they take half the
+// registers (8 vectors of bf16 a thread spilled 0.5 KB a thread without it).
+template <class V, int N>
+__device__ __forceinline__ void forget_unpacked(V (&v)[N]) {
+#pragma unroll
+    for (int q = 0; q < N; ++q)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) asm volatile("" : "+r"(v[q].u[e]));
+}
+
+// A row is cut into 2^parts_log2 equal parts, one block each; the blocks of a row form a cluster and exchange their maxima and
+// sums through distributed shared memory (the gradient alone needs no exchange).  A block goes through its part in batches of
+// NV vectors a thread.  Where loss and gradient are both wanted it goes back through the batches: the last is still in registers, the
+// first was put aside in shared memory (every thread reads what it wrote itself), those between are read again, youngest
+// first, from L2.
+constexpr int NV = 8;
+
 template <class T, int THREADS, int MODE>
-__global__ void __launch_bounds__(THREADS) distill_kernel(const DistillArgs a) {
-    constexpr int W = Row<T>::W, WARPS = THREADS / 32;
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const DistillArgs a, const int parts_log2) {
+    constexpr int W = Part<T>::W, WARPS = THREADS / 32, BATCH = NV * THREADS;
+    extern __shared__ uint4 s_first[];                             // [NV][THREADS]: the first batch
     __shared__ int s_idx[MAX_TOP];
     __shared__ float s_p[MAX_TOP], s_z[MAX_TOP];
-    __shared__ float s_max[WARPS], s_sum[WARPS];
+    __shared__ float2 s_stat[WARPS];                               // (maximum, sum) of each warp
     __shared__ Teacher s_teacher;
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const size_t t = blockIdx.x;
+    const int parts = 1 << parts_log2, part = (int)(blockIdx.x & (unsigned)(parts - 1));
+    const size_t t = blockIdx.x >> parts_log2;
     const T* z = static_cast<const T*>(a.logits) + t * a.stride;
     T* dz = MODE == MODE_LOSS ? nullptr : static_cast<T*>(a.grad) + t * a.grad_stride;
-    const Row<T> row(z, a.V);
-    const bool aligned = MODE != MODE_LOSS && ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(dz)) & 15u) == 0;
-    const size_t n = row.vectors();
+    const Part<T> mine(z, (int)a.V, part, parts_log2, tid);
+    const uint32_t last = mine.n == 0 ? 0 : (mine.n - 1) / BATCH * BATCH;      // first vector of the last batch
     const float c = a.inv_tau * LOG2E;
+    raw_vec<T, W> v[NV];
+    auto load = [&](uint32_t i0, bool again) {                     // vectors i0 + tid, i0 + tid + THREADS, ...; -inf past the end
+#pragma unroll
+        for (int q = 0; q < NV; ++q) {
+            const uint32_t i = i0 + q * THREADS + tid;
+            if (i < mine.n) {
+                v[q] = again ? load_again<T, W>(mine.p + (size_t)i * W) : load_raw<T, W>(mine.p + (size_t)i * W);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[q].u[e] = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;
+            }
+        }
+    };
+    load(0, MODE == MODE_STEP);
+    const float edge = mine.edge >= 0 ? unpack_one<T>(z[mine.edge]) : -INFINITY;
     float weight = a.weight != nullptr ? a.weight[t] : 1.0f;
     if (MODE == MODE_GRAD && a.dloss != nullptr) weight *= a.dloss[t];
+    if (w == 0) teacher_row<T>(a, t, z, mine.col0, mine.col1, lane, s_idx, s_p, s_z, &s_teacher);
 
-    if (w == 0) teacher_row<T>(a, t, z, 0, a.V, lane, s_idx, s_p, s_z, &s_teacher);
-    float M, S;                          // largest logit, sum of exponentials below it
+    float M = 0.0f, S = 1.0f, list = 0.0f;                         // largest logit, sum of exponentials below it, teacher's part of the loss
     if (MODE == MODE_GRAD) {
         __syncthreads();
     } else {
         float m = -INFINITY, s = 0.0f;
-        if (weight != 0.0f)
-            for (size_t i = tid; i < n; i += THREADS) {
-                float x[W];
-                unpack<T, W>(row.load(i), x);
-                float top = x[0];
+        for (uint32_t i0 = 0;;) {
+            if (MODE == MODE_STEP && i0 == 0 && last > 0) {
 #pragma unroll
-                for (int e = 1; e < W; ++e) top = fmaxf(top, x[e]);
-                const float m2 = fmaxf(m, top);
-                const Below below(c, m2);
-                float add = 0.0f;
-#pragma unroll
-                for (int e = 0; e < W; ++e) add += below(x[e]);
-                s = s * ex2((m - below.m) * c) + add;
-                m = m2;
+                for (int q = 0; q < NV; ++q) s_first[q * THREADS + tid] = make_uint4(v[q].u[0], v[q].u[1], v[q].u[2], v[q].u[3]);
             }
+            const float m2 = max_of<T, NV>(v, m), ref = m2 == -INFINITY ? 0.0f : m2;
+            forget_unpacked(v);
+            s = s * ex2((m - ref) * c) + sum_below<T, NV>(v, c, ref);
+            m = m2;
+            if (i0 >= last) break;
+            i0 += BATCH;
+            load(i0, MODE == MODE_STEP);
+        }
+        if (mine.edge >= 0) join(m, s, edge, edge == -INFINITY ? 0.0f : edge == edge ? 1.0f : edge, c);
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) join(m, s, __shfl_xor_sync(0xffffffffu, m, d), __shfl_xor_sync(0xffffffffu, s, d), c);
-        if (lane == 0) { s_max[w] = m; s_sum[w] = s; }
-        __syncthreads();
-        M = s_max[0];
-        S = s_sum[0];
-        for (int q = 1; q < WARPS; ++q) join(M, S, s_max[q], s_sum[q], c);
+        if (lane == 0) s_stat[w] = make_float2(m, s);
+        // every warp joins the statistics of all warps of the row for itself, in one order
+        m = -INFINITY; s = 0.0f;
+        if (parts == 1) {
+            __syncthreads();
+            if (lane < WARPS) { m = s_stat[lane].x; s = s_stat[lane].y; }
+            list = s_teacher.part;
+        } else {
+            cluster_arrive();
+            cluster_wait();
+            for (int i = lane; i < parts * WARPS; i += 32) {
+                const float2 x = peer(&s_stat[i % WARPS], i / WARPS);
+                join(m, s, x.x, x.y, c);
+            }
+            if (part == 0 && w == 0) list = warp_sum(lane < parts ? peer(reinterpret_cast<const float2*>(&s_teacher), lane).y : 0.0f);
+            cluster_arrive();                                      // (this block has read its peers' shared memory)
+        }
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) join(m, s, __shfl_xor_sync(0xffffffffu, m, d), __shfl_xor_sync(0xffffffffu, s, d), c);
+        // (a join is not symmetric to the last bit: all threads take lane 0's result, the same in every warp and block)
+        M = __shfl_sync(0xffffffffu, m, 0);
+        S = __shfl_sync(0xffffffffu, s, 0);
     }
     const float mass = s_teacher.mass, lse = MODE == MODE_GRAD ? a.lse[t] : fmaf(M, a.inv_tau, logf(S));
     const bool skip = weight == 0.0f || s_teacher.any == 0 || (MODE == MODE_GRAD ? lse : M) == -INFINITY;   // nothing to learn from this row
-    if (MODE != MODE_GRAD && tid == 0) {
-        a.loss[t] = skip ? 0.0f : weight * (s_teacher.part + mass * lse);
+    if (MODE != MODE_GRAD && part == 0 && tid == 0) {
+        a.loss[t] = skip ? 0.0f : weight * (list + mass * lse);
         a.lse[t] = skip ? -INFINITY : lse;
     }
-    if (MODE == MODE_LOSS) return;
-    // m exp(u - lse) g = G exp2(c z - off)
-    const float g = weight * a.inv_tau;
-    float G, off;
-    bool fused;
-    if (MODE == MODE_GRAD) {                                       // off = lse log2 e, its rounding error moved into G
-        off = lse * LOG2E;
-        fused = fabsf(off) < 1e38f;
-        G = g * mass * (fused ? ex2(-(fmaf(lse, LOG2E, -off) + lse * LOG2E_REST)) : 1.0f);
-    } else {
-        off = c * M;
-        fused = fabsf(off) < 1e38f;
-        G = g * mass / S;
-    }
-    auto scaled = [&](float x) {
-        if (fused) return G * ex2(fmaf(x, c, -off));
-        return G * ex2(MODE == MODE_GRAD ? fmaf(x, a.inv_tau, -lse) * LOG2E : (x - M) * c);
-    };
-    for (size_t i = tid; i < n; i += THREADS) {
-        float x[W];
-        if (skip) {
-#pragma unroll
-            for (int e = 0; e < W; ++e) x[e] = 0.0f;
+    if (MODE != MODE_LOSS) {
+        T* dst = dz + mine.col;
+        const bool aligned = (reinterpret_cast<uintptr_t>(dst) & 15u) == 0;
+        // m exp(u - lse) g = G exp2(c z - off)
+        const float g = weight * a.inv_tau;
+        float G, off;
+        bool fused;
+        if (MODE == MODE_GRAD) {                                   // off = lse log2 e, its rounding error moved into G
+            off = lse * LOG2E;
+            fused = fabsf(off) < 1e38f;
+            G = g * mass * (fused ? ex2(-(fmaf(lse, LOG2E, -off) + lse * LOG2E_REST)) : 1.0f);
         } else {
-            unpack<T, W>(row.load(i), x);
-#pragma unroll
-            for (int e = 0; e < W; ++e) x[e] = scaled(x[e]);
+            off = c * M;
+            fused = fabsf(off) < 1e38f;
+            G = g * mass / S;
         }
-        store_row<T>(row, dz, aligned, i, x);
+        if (skip) fused = false;
+        auto scaled = [&](float x) {
+            if (fused) return G * ex2(fmaf(x, c, -off));
+            return G * ex2(MODE == MODE_GRAD ? fmaf(x, a.inv_tau, -lse) * LOG2E : (x - M) * c);
+        };
+        for (uint32_t step = 0; step <= last; step += BATCH) {
+            // the gradient alone: batch 0 (already there), 1, 2, ...; after the loss: the last (still there), ..., 1, and 0 from shared memory
+            const uint32_t i0 = MODE == MODE_STEP ? last - step : step;
+            if (step > 0 && !skip) {
+                if (MODE == MODE_STEP && i0 == 0) {
+#pragma unroll
+                    for (int q = 0; q < NV; ++q) {
+                        const uint4 u = s_first[q * THREADS + tid];
+                        v[q].u[0] = u.x; v[q].u[1] = u.y; v[q].u[2] = u.z; v[q].u[3] = u.w;
+                    }
+                } else {
+                    load(i0, false);
+                }
+            }
+            forget_unpacked(v);
+#pragma unroll
+            for (int q = 0; q < NV; ++q) {
+                const uint32_t i = i0 + q * THREADS + tid;
+                if (i < mine.n) {
+                    float x[W];
+                    unpack<T, W>(v[q], x);
+                    if (fused) {
+#pragma unroll
+                        for (int e = 0; e < W; ++e) x[e] = G * ex2(fmaf(x[e], c, -off));
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < W; ++e) x[e] = skip ? 0.0f : scaled(x[e]);
+                    }
+                    if (aligned) {
+                        store_vec<T, W>(dst + (size_t)i * W, x);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < W; ++e) {
+                            const float one[1] = {x[e]};
+                            store_vec<T, 1>(dst + (size_t)i * W + e, one);
+                        }
+                    }
+                }
+            }
+        }
+        if (mine.edge >= 0) {
+            const float one[1] = {skip ? 0.0f : scaled(edge)};
+            store_vec<T, 1>(dz + mine.edge, one);
+        }
+        if (!skip) {                                               // the listed columns, behind the stores of all threads
+            __syncthreads();
+            for (int k = tid; k < a.K; k += THREADS) {
+                const int i = s_idx[k];
+                if (i < mine.col0 || i >= mine.col1) continue;     // (an absent entry is -1)
+                float p = 0.0f;                                    // an index that is listed twice: both count
+                for (int q = 0; q < a.K; ++q) p += s_idx[q] == i ? s_p[q] : 0.0f;
+                const float d[1] = {scaled(s_z[k]) - g * p};
+                store_vec<T, 1>(dz + i, d);
+            }
+        }
     }
-    if (skip) return;
-    __syncthreads();
-    for (int k = tid; k < a.K; k += THREADS) {
-        const int i = s_idx[k];
-        if (i < 0) continue;
-        float p = 0.0f;                                    // an index that is listed twice: both count
-        for (int q = 0; q < a.K; ++q) p += s_idx[q] == i ? s_p[q] : 0.0f;
-        const float d[1] = {scaled(s_z[k]) - g * p};
-        store_vec<T, 1>(dz + i, d);
+    if (MODE != MODE_GRAD && parts > 1) cluster_wait();            // no block goes while another may still read its shared memory
+}
+
+template <class T, int THREADS, int MODE>
+int launch_parts(const DistillArgs& a, size_t rows, int parts_log2, size_t vectors, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1u << parts_log2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = MODE != MODE_GRAD && parts_log2 > 0 ? 1 : 0; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(rows << parts_log2)); cfg.blockDim = dim3(THREADS);
+    if (MODE == MODE_STEP && vectors > NV * THREADS) cfg.dynamicSmemBytes = NV * THREADS * 16;
+    if (cfg.dynamicSmemBytes > 48 * 1024) {
+        static std::atomic<uint64_t> ready{0};                     // devices on which the shared-memory limit is raised
+        int dev = 0;
+        EC_CUDA(cudaGetDevice(&dev));
+        if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1u)) {
+            EC_CUDA(cudaFuncSetAttribute(distill_kernel<T, THREADS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, NV * THREADS * 16));
+            if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
+    }
+    EC_CUDA(cudaLaunchKernelEx(&cfg, distill_kernel<T, THREADS, MODE>, a, parts_log2));
+    return EC_OK;
+}
+
+template <class T, int MODE>
+int launch_rows(const DistillArgs& a, size_t rows, cudaStream_t st) {
+    constexpr int W = 16 / (int)sizeof(T);
+    const size_t n = (a.V + W - 1) / W;                            // vectors of a row, at most
+    int pl = 0;
+    auto per = [&] { return (n + ((size_t)1 << pl) - 1) >> pl; };
+    while (pl < 3 && (rows << (pl + 1)) <= 296 && per() > 512) ++pl;          // few rows: more blocks each
+    if (MODE == MODE_GRAD) {
+        // nothing joins the parts: parts of 32 KB (4096 x 32768 bf16: 95 us, 99 in one part, 98 in four)
+        while (pl < 3 && per() > 2048) ++pl;
+    }
+    if (MODE != MODE_STEP) {
+        // rows up to 24 KB: smaller blocks, more rows on an SM (16384 x 8192 bf16, loss: 66 us with 64 threads, 71 with 128; from
+        // 64 KB on 101 and 97)
+        if (per() <= 64 * 24) return launch_parts<T, 64, MODE>(a, rows, pl, per(), st);
+        return launch_parts<T, 128, MODE>(a, rows, pl, per(), st);
+    } else {
+        // Few threads: many rows on an SM, but more batches between the first (shared memory) and the last (registers) that are
+        // read twice; rows of up to 16 vectors a thread are read once.  Long rows re-read their middle, and from 256 KB on take two blocks, so that what is re-read is still
+        // in L2.  Measured, us with 64 / 128 / 256 / 512 threads: 16384 x 4099 fp32 104 / 122 / 172 / 298; 8192 x 32768 bf16
+        // 242 / 210 / 205 / 249; 4096 x 65536 268 / 235 / 203 / 213; 2048 x 131072 284 / 261 / 234 / 210.
+        while (pl < 3 && per() > 512 * 33) ++pl;
+        if (per() <= 64 * 24) return launch_parts<T, 64, MODE>(a, rows, pl, per(), st);
+        if (per() <= 128 * 24) return launch_parts<T, 128, MODE>(a, rows, pl, per(), st);
+        if (per() <= 256 * 40) return launch_parts<T, 256, MODE>(a, rows, pl, per(), st);
+        return launch_parts<T, 512, MODE>(a, rows, pl, per(), st);
     }
 }
 
 template <int MODE>
 int launch_distill(const DistillArgs& a, size_t T, ec_dtype_t dtype, cudaStream_t st) {
-    if (dtype == EC_F32) distill_kernel<float, 512, MODE><<<(unsigned)T, 512, 0, st>>>(a);
-    else distill_kernel<bf16_t, 512, MODE><<<(unsigned)T, 512, 0, st>>>(a);
-    EC_CUDA(cudaGetLastError());
-    return EC_OK;
+    return dtype == EC_F32 ? launch_rows<float, MODE>(a, T, st) : launch_rows<bf16_t, MODE>(a, T, st);
 }
 
 int check(const DistillArgs& a, size_t T, ec_dtype_t dtype, ec_index_t index, ec_dtype_t top_dtype, float temperature, int mode) {
-    if (T > 0x7ffffffeull || a.V < 1 || a.V > 0x7ffffffeull || a.K < 1 || !(temperature > 0.0f) || !(temperature < INFINITY)) return EC_ERR_INVALID;
+    if (T > 0x7ffffffeull || a.V < 1 || a.V > MAX_V || a.K < 1 || !(temperature > 0.0f) || !(temperature < INFINITY)) return EC_ERR_INVALID;
     if (a.stride < a.V || (mode != MODE_LOSS && a.grad_stride < a.V) || (index != EC_INDEX_32 && index != EC_INDEX_64)) return EC_ERR_INVALID;
     if (T > 0 && (!a.logits || !a.top_index || !a.top_logit || !a.lse || (mode != MODE_GRAD && !a.loss) || (mode != MODE_LOSS && !a.grad)))
         return EC_ERR_INVALID;

@@ -39,6 +39,17 @@ __device__ __forceinline__ raw_vec<T, W> load_raw(const T* p) {          // read
     }
     return r;
 }
+// the same for rows that will be read again soon: they should stay in L2
+template <class T, int W>
+__device__ __forceinline__ raw_vec<T, W> load_again(const T* p) {
+    static_assert(sizeof(T) * W == 16, "16 bytes");
+    uint64_t pol;
+    asm volatile("createpolicy.fractional.L2::evict_last.b64 %0, 1.0;" : "=l"(pol));
+    const uint4 v = ld_stream16(p, pol);
+    raw_vec<T, W> r;
+    r.u[0] = v.x; r.u[1] = v.y; r.u[2] = v.z; r.u[3] = v.w;
+    return r;
+}
 template <class T, int W>
 __device__ __forceinline__ void unpack(const raw_vec<T, W>& r, float (&x)[W]) {
     if constexpr (sizeof(T) == 4) {
