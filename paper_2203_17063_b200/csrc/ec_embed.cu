@@ -4,12 +4,14 @@
 // written), nothing to reuse but L2.
 //
 // Gradient: grad[v] = scale * sum of dout[t] over token[t] = v.  The tokens are sorted (stable, so a row's positions stay in
-// ascending order), then the sorted tokens and the table's rows are walked together as one path of T + V steps: a token
-// step adds a row of dout to the running sum, a row step writes the sum out and starts the next.  Token p of the sorted order
-// is step p + key[p] of the path, so the path is cut into equal shares by a search for the share's first step; every row of
-// dout is read once, every row of grad written once, and a token that makes up a tenth of the text is spread over as many
-// shares as it takes.  A row that crosses the border of a share leaves partial sums in fp32, joined in share order by a second
-// small kernel: no atomics on values, the same bits every run.
+// ascending order), then the sorted tokens and the table's rows are laid out as one path of T + V steps: a token step reads a
+// row of dout, a row step writes a row of grad.  Token p of the sorted order is step p + key[p] of the path, so the path is
+// cut into equal stretches, a block each, by a search for a stretch's first step; every row of dout is read once, every row of
+// grad written once, and a token that makes up a tenth of the text is spread over as many blocks as it takes.  A row that
+// crosses the border between two shares leaves partial sums in fp32, joined in share order by a second small kernel: no
+// atomics on values, the same bits every run.
+
+#include <atomic>
 
 #include "ec_vec.cuh"
 
@@ -57,20 +59,32 @@ lookup_kernel(const TI* __restrict__ table, size_t table_stride, size_t V, size_
     }
 }
 
+// The widest unit (1, 2, 4 or, for bf16 input, 8 elements) that the row length and both sides' alignment allow.
+template <class TI, class TO>
+int unit_of(size_t D, const void* in, size_t in_stride, const void* out, size_t out_stride) {
+    for (int u = sizeof(TI) == 2 ? 8 : 4; u > 1; u /= 2)
+        if (D % u == 0 && rows_aligned(in, in_stride, sizeof(TI), u) && rows_aligned(out, out_stride, sizeof(TO), u)) return u;
+    return 1;
+}
+
 template <class IDX, class TI, class TO>
 int launch_lookup(const void* table, size_t V, size_t D, size_t ts, const void* tokens, size_t T, float scale, void* out,
                   size_t os, cudaStream_t st) {
-    constexpr int W = sizeof(TI) == 2 ? 8 : 4;
-    const bool vec = D % W == 0 && rows_aligned(table, ts, sizeof(TI), W) && rows_aligned(out, os, sizeof(TO), W);
+    const int u = unit_of<TI, TO>(D, table, ts, out, os);
     const unsigned gx = (unsigned)((T + LK_THREADS / 32 - 1) / (LK_THREADS / 32));
-    const size_t per = 32 * (size_t)(vec ? W : 1) * LK_INFLIGHT, pieces = (D + per - 1) / per;
+    const size_t per = 32 * (size_t)u * LK_INFLIGHT, pieces = (D + per - 1) / per;
     const dim3 grid(gx, (unsigned)(pieces < 64 ? pieces : 64));
-    if (vec)
-        lookup_kernel<IDX, TI, TO, W><<<grid, LK_THREADS, 0, st>>>((const TI*)table, ts, V, D, (const IDX*)tokens, T, scale, (TO*)out, os);
-    else
-        lookup_kernel<IDX, TI, TO, 1><<<grid, LK_THREADS, 0, st>>>((const TI*)table, ts, V, D, (const IDX*)tokens, T, scale, (TO*)out, os);
-    EC_CUDA(cudaGetLastError());
-    return EC_OK;
+    auto launch = [&](auto kernel) {
+        kernel<<<grid, LK_THREADS, 0, st>>>((const TI*)table, ts, V, D, (const IDX*)tokens, T, scale, (TO*)out, os);
+        EC_CUDA(cudaGetLastError());
+        return (int)EC_OK;
+    };
+    if constexpr (sizeof(TI) == 2) {
+        if (u == 8) return launch(lookup_kernel<IDX, TI, TO, 8>);
+    }
+    if (u == 4) return launch(lookup_kernel<IDX, TI, TO, 4>);
+    if (u == 2) return launch(lookup_kernel<IDX, TI, TO, 2>);
+    return launch(lookup_kernel<IDX, TI, TO, 1>);
 }
 
 // ---- sorting the tokens ------------------------------------------------------------------------------------------
@@ -207,36 +221,176 @@ __global__ void __launch_bounds__(SORT_THREADS) sort_scatter_kernel(const SortAr
     }
 }
 
+// Up to 65536 tokens: the whole sort in one launch, by one cluster of 1 to 8 blocks.  A thread keeps its items in registers; a
+// pass ranks them inside the block, the blocks exchange their digit counts, and every item is sent to its place in some
+// block's shared memory (the last pass: in global memory).
+constexpr int CS_THREADS = 512, CS_WARPS = CS_THREADS / 32, CS_MAX_ITEMS = 16;
+
+struct ClusterSortArgs {
+    const void* tokens;
+    uint32_t* keys; uint32_t* pos;
+    uint32_t* joins;
+    uint32_t T, V;
+    long long skip;
+    int bits, passes;
+};
+
+__device__ __forceinline__ void sort_cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t peer_address(const void* p, uint32_t rank) {
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ uint32_t peer_load(uint32_t address) {
+    uint32_t x;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(address) : "memory");
+    return x;
+}
+__device__ __forceinline__ void peer_store(uint32_t address, uint32_t x, uint32_t y) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(address), "r"(x), "r"(y) : "memory");
+}
+
+template <class IDX, int ITEMS>
+__global__ void __launch_bounds__(CS_THREADS) sort_cluster_kernel(const ClusterSortArgs a) {
+    grid_dependency_wait();
+    extern __shared__ uint2 s_items[];                             // [ITEMS * CS_THREADS]: items of the next pass
+    __shared__ uint32_t s_n[CS_WARPS][SORT_BINS];
+    __shared__ uint32_t s_total[SORT_BINS], s_base[SORT_BINS], s_warp[CS_WARPS];
+    constexpr uint32_t HOLD = ITEMS * CS_THREADS;                  // items of a block (a power of two)
+    const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
+    const uint32_t rank = blockIdx.x, blocks = gridDim.x;          // (one cluster: a block's number is its rank)
+    const uint32_t base = rank * HOLD + w * (32 * ITEMS) + lane;   // (warp, step, lane) is the items' order
+    if (rank == 0 && tid == 0) *a.joins = 0;
+    uint32_t key[ITEMS], pos[ITEMS], at[ITEMS];
+#pragma unroll
+    for (int q = 0; q < ITEMS; ++q) {
+        const uint32_t i = base + q * 32;
+        key[q] = i < a.T ? token_key(static_cast<const IDX*>(a.tokens), i, a.V, a.skip) : 0u;
+        pos[q] = i;
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * a.bits;
+        const uint32_t bins = 1u << a.bits;
+        for (int d = tid; d < CS_WARPS * SORT_BINS; d += CS_THREADS) (&s_n[0][0])[d] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            const bool in = base + q * 32 < a.T;
+            const uint32_t d = in ? (key[q] >> shift) & (bins - 1) : bins;      // items past the end: a digit of their own
+            const uint32_t same = __match_any_sync(0xffffffffu, d);
+            const uint32_t below = __popc(same & ((1u << lane) - 1u));
+            const uint32_t old = in ? s_n[w][d] : 0u;
+            __syncwarp();
+            if (in && below == 0) s_n[w][d] = old + __popc(same);
+            __syncwarp();
+            at[q] = old + below;
+        }
+        __syncthreads();
+        if (tid < (int)bins) {                                     // a thread per digit: the warps' counts become their offsets
+            uint32_t sum = 0;
+#pragma unroll
+            for (int q = 0; q < CS_WARPS; ++q) {
+                const uint32_t n = s_n[q][tid];
+                s_n[q][tid] = sum;
+                sum += n;
+            }
+            s_total[tid] = sum;
+        }
+        sort_cluster_sync();
+        uint32_t before = 0, all = 0;
+        if (tid < (int)bins)
+            for (uint32_t r = 0; r < blocks; ++r) {
+                const uint32_t n = peer_load(peer_address(&s_total[tid], r));
+                before += r < rank ? n : 0u;
+                all += n;
+            }
+        const uint32_t inc = warp_inclusive(all, lane);
+        if (lane == 31) s_warp[w] = inc;
+        __syncthreads();
+        for (int q = 0; q < w; ++q) before += s_warp[q];
+        if (tid < (int)bins) s_base[tid] = before + inc - all;
+        __syncthreads();
+        const bool last = pass + 1 == a.passes;
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q) {
+            if (base + q * 32 >= a.T) continue;
+            const uint32_t d = (key[q] >> shift) & (bins - 1), p = s_base[d] + s_n[w][d] + at[q];
+            if (last) {
+                a.keys[p] = key[q];
+                a.pos[p] = pos[q];
+            } else {
+                peer_store(peer_address(&s_items[p % HOLD], p / HOLD), key[q], pos[q]);
+            }
+        }
+        sort_cluster_sync();                                       // (the last one: no block goes while another may read its counts)
+        if (!last) {
+#pragma unroll
+            for (int q = 0; q < ITEMS; ++q) {
+                const uint2 x = s_items[w * (32 * ITEMS) + q * 32 + lane];
+                key[q] = x.x;
+                pos[q] = x.y;
+            }
+        }
+    }
+}
+
+template <class IDX, int ITEMS>
+int launch_cluster_sort(const ClusterSortArgs& a, unsigned blocks, cudaStream_t st) {
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = blocks; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 2; cfg.stream = st;
+    cfg.gridDim = dim3(blocks); cfg.blockDim = dim3(CS_THREADS);
+    cfg.dynamicSmemBytes = (size_t)ITEMS * CS_THREADS * 8;
+    if (cfg.dynamicSmemBytes > 8 * 1024) {                         // (beside 37 KB of static shared memory)
+        static std::atomic<uint64_t> ready{0};                     // devices on which the limit is raised
+        int dev = 0;
+        EC_CUDA(cudaGetDevice(&dev));
+        if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1u)) {
+            EC_CUDA(cudaFuncSetAttribute(sort_cluster_kernel<IDX, ITEMS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg.dynamicSmemBytes));
+            if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+        }
+    }
+    EC_CUDA(cudaLaunchKernelEx(&cfg, sort_cluster_kernel<IDX, ITEMS>, a));
+    return EC_OK;
+}
+
 // ---- the walk ----------------------------------------------------------------------------------------------------
 
 constexpr int GR_THREADS = 256;
-constexpr int GR_INFLIGHT = 8;          // rows of dout a thread has in flight
+constexpr int GR_INFLIGHT = 8;          // rows of dout a thread has in flight (131072 x 2048: 303 us; four: 313; eight in 64 registers: 312)
 constexpr int GR_MAX_SHARE = 64;
-constexpr int GR_TOKENS = 1024;         // most path steps of a block
+constexpr int GR_STEPS = 1024;          // most path steps of a block
+constexpr int GR_LONG = 32;             // a row with this many tokens before a share's border is cut there; a shorter one goes to the next share
+constexpr uint32_t NO_ROW = 0xffffffffu;
 
-// How a call is cut: groups of G threads take shares of C path steps; a block holds GR_THREADS / G groups.
+// How a call is cut: a block takes C path steps for each of its GR_THREADS / G groups; a group's share of its tokens is even.
 struct GradPlan {
-    int W, G, C;                        // elements per thread, threads per group, steps per share
+    int U, G, C;                        // elements a unit, threads a group, path steps a group
     unsigned shares, blocks, slices;    // shares = groups in all (a multiple of the groups of a block)
 };
 
-GradPlan grad_plan(size_t T, size_t V, size_t D, int W) {
+// W: elements a thread takes of a row, as W / U units G units apart
+GradPlan grad_plan(size_t T, size_t V, size_t D, int U, int W) {
     GradPlan p;
-    p.W = W;
+    p.U = U;
     const size_t lanes = (D + W - 1) / W;
     p.G = 8;
     while (p.G < GR_THREADS && (size_t)p.G < lanes) p.G *= 2;
     p.slices = (unsigned)((lanes + p.G - 1) / p.G);
     const unsigned groups = GR_THREADS / p.G;
     const size_t steps = T + V;
-    p.C = GR_TOKENS / (int)groups < GR_MAX_SHARE ? GR_TOKENS / (int)groups : GR_MAX_SHARE;
+    p.C = GR_STEPS / (int)groups < GR_MAX_SHARE ? GR_STEPS / (int)groups : GR_MAX_SHARE;
     while (p.C > 8 && (steps / ((size_t)p.C * groups)) * p.slices < 148 * 8) p.C /= 2;
     p.blocks = (unsigned)((steps + (size_t)p.C * groups - 1) / ((size_t)p.C * groups));
     p.shares = p.blocks * groups;
     return p;
 }
-
-constexpr uint32_t NO_ROW = 0xffffffffu;
 
 struct GradArgs {
     const uint32_t* keys; const uint32_t* pos;      // sorted tokens, their positions
@@ -250,8 +404,10 @@ struct GradArgs {
     int G, C, accumulate;
 };
 
-// Number of sorted tokens p with p + key[p] < d: the tokens among the first d steps of the path.  One warp, 33 sections at a time.
-__device__ __forceinline__ uint32_t path_search(const uint32_t* __restrict__ keys, uint32_t T, uint32_t V, uint32_t d, int lane) {
+// Where the border of a block at path step d lies: number of sorted tokens before it and row.  That is the tokens p with
+// p + key[p] < d, found by one warp, 33 sections at a time - moved back to a row's first token if the border falls between
+// two tokens of the row and fewer than GR_LONG of them lie before it, so that only long rows are cut and joined later.
+__device__ __forceinline__ void border(const uint32_t* __restrict__ keys, uint32_t T, uint32_t V, uint32_t d, int lane, uint32_t* tokens, uint32_t* row) {
     uint32_t lo = d > V ? d - V : 0u, hi = d < T ? d : T;
     while (lo < hi) {
         const uint32_t step = (hi - lo + 31) / 32, p = lo + lane * step;
@@ -262,122 +418,210 @@ __device__ __forceinline__ uint32_t path_search(const uint32_t* __restrict__ key
         lo = lo + (n - 1) * step + 1;
         hi = top < hi ? top : hi;
     }
-    return lo;
+    const uint32_t j = d - lo;
+    const uint32_t same = __ballot_sync(0xffffffffu, lo < T && lo > (uint32_t)lane && keys[lo] == j && keys[lo - 1 - lane] == j);
+    static_assert(GR_LONG == 32, "one look back of a warp");
+    *tokens = same == 0xffffffffu ? lo : lo - (uint32_t)(__ffs(~same) - 1);
+    *row = j;
 }
 
-template <class TO, int W>
-__device__ __forceinline__ void write_row(TO* p, float (&acc)[W], float scale, bool add) {
-    float x[W];
+// n zeros from p on by one warp, in 16-byte pieces wherever p lies
+template <class TO>
+__device__ __forceinline__ void zero_span(TO* p, size_t n, uint32_t lane) {
+    constexpr uint32_t W = 16 / sizeof(TO);
+    const uint32_t off = (uint32_t)(reinterpret_cast<uintptr_t>(p) & 15u) / (uint32_t)sizeof(TO);
+    const size_t head = off == 0 ? 0 : W - off < n ? W - off : n, vecs = (n - head) / W;
+    const uint32_t rest = (uint32_t)(n - head - vecs * W);
+    const float zero[1] = {0.0f};
+    uint4* q = reinterpret_cast<uint4*>(p + head) + lane;
+    if (lane < head) store_vec<TO, 1>(p + lane, zero);
+    if (lane < rest) store_vec<TO, 1>(p + head + vecs * W + lane, zero);
+#pragma unroll 4
+    for (size_t i = lane; i < vecs; i += 32, q += 32) __stcs(q, make_uint4(0u, 0u, 0u, 0u));
+}
+
+template <class TO, int U>
+__device__ __forceinline__ void write_unit(TO* p, const float* acc, float scale, bool add) {
+    float x[U];
 #pragma unroll
-    for (int e = 0; e < W; ++e) x[e] = scale * acc[e] + 0.0f;      // (+0 for a row without tokens, whatever the scale's sign)
+    for (int e = 0; e < U; ++e) x[e] = scale * acc[e];
     if (add) {
-        float old[W];
-        if constexpr (sizeof(TO) * W > 16) {
-            constexpr int H = W / 2;
+        float old[U];
+        if constexpr (sizeof(TO) * U > 16) {
+            constexpr int H = U / 2;
             float a[H], b[H];
             load_vec<TO, H>(p, a);
             load_vec<TO, H>(p + H, b);
 #pragma unroll
             for (int e = 0; e < H; ++e) { old[e] = a[e]; old[H + e] = b[e]; }
         } else {
-            load_vec<TO, W>(p, old);
+            load_vec<TO, U>(p, old);
         }
 #pragma unroll
-        for (int e = 0; e < W; ++e) x[e] += old[e];
+        for (int e = 0; e < U; ++e) x[e] += old[e];
     }
-    store_vec<TO, W>(p, x);
+    store_vec<TO, U>(p, x);
 }
 
-template <class TI, class TO, int W>
-__global__ void __launch_bounds__(GR_THREADS) grad_walk_kernel(const GradArgs a, const TI* __restrict__ dout, TO* __restrict__ grad) {
+// A block takes a stretch of the path: its rows without tokens are written with zeros by the warps in turn, its tokens are shared
+// out evenly to the groups.
+template <class TI, class TO, int U, int NU>
+__global__ void __launch_bounds__(GR_THREADS, 3) grad_walk_kernel(const GradArgs a, const TI* __restrict__ dout, TO* __restrict__ grad) {
     grid_dependency_wait();
-    __shared__ uint32_t s_key[GR_TOKENS + 1], s_pos[GR_TOKENS];      // s_key[0]: the token before the block's first
-    __shared__ uint32_t s_cut[2];
+    __shared__ uint32_t s_key[GR_STEPS + GR_LONG + 2], s_pos[GR_STEPS + GR_LONG];      // s_key[0], s_key[n + 1]: the tokens before and behind the block's
+    __shared__ uint32_t s_has[(GR_STEPS + GR_LONG) / 32 + 1];                          // bit r: row rows0 + r has tokens
+    __shared__ uint32_t s_tok[2], s_rowat[2];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const uint32_t groups = GR_THREADS / a.G, total = a.T + a.V;
     const uint32_t d0 = blockIdx.x * groups * a.C, d1 = d0 + groups * a.C < total ? d0 + groups * a.C : total;
     if (w < 2) {
-        const uint32_t i = path_search(a.keys, a.T, a.V, w == 0 ? d0 : d1, lane);
-        if (lane == 0) s_cut[w] = i;
+        uint32_t i, j;
+        border(a.keys, a.T, a.V, w == 0 ? d0 : d1, lane, &i, &j);
+        if (lane == 0) { s_tok[w] = i; s_rowat[w] = j; }
+    } else {
+        for (uint32_t q = tid - 64; q < sizeof(s_has) / 4; q += GR_THREADS - 64) s_has[q] = 0;
     }
     __syncthreads();
-    const uint32_t i0 = s_cut[0], n = s_cut[1] - i0;
-    if (tid == 0) s_key[0] = i0 > 0 ? a.keys[i0 - 1] : 0xffffffffu;
-    for (uint32_t q = tid; q < n; q += GR_THREADS) {
-        s_key[q + 1] = a.keys[i0 + q];
-        s_pos[q] = a.pos[i0 + q];
+    const uint32_t i0 = s_tok[0], n = s_tok[1] - i0, row0 = s_rowat[0], row1 = s_rowat[1];
+    for (uint32_t q = tid; q < n + 2; q += GR_THREADS) {
+        const uint32_t k = i0 + q > 0 && i0 + q <= a.T ? a.keys[i0 + q - 1] : NO_ROW;
+        s_key[q] = k;
+        if (q > 0 && q <= n) s_pos[q - 1] = a.pos[i0 + q - 1];
+        if (k >= row0 && k < row1) atomicOr(&s_has[(k - row0) >> 5], 1u << ((k - row0) & 31));      // (bits: order is free)
     }
     __syncthreads();
 
-    const uint32_t g = tid / a.G;
-    const uint32_t b = d0 + g * a.C < total ? d0 + g * a.C : total, e = b + a.C < total ? b + a.C : total;   // the share's steps
-    uint32_t lo = 0, hi = n;
-    while (lo < hi) {                                                // tokens of the block before the share
-        const uint32_t m = (lo + hi) / 2;
-        if (i0 + m + s_key[m + 1] < b) lo = m + 1; else hi = m;
-    }
-    uint32_t i = lo;
-    hi = n;
-    while (lo < hi) {
-        const uint32_t m = (lo + hi) / 2;
-        if (i0 + m + s_key[m + 1] < e) lo = m + 1; else hi = m;
-    }
-    const uint32_t i_end = lo;
-    uint32_t j = b - (i0 + i);
-    const uint32_t j_end = e - (i0 + i_end);
-    const uint32_t share = blockIdx.x * groups + g;
-    const bool inside = j < a.V && s_key[i] == j;                    // the row goes on from the share before
-    const size_t c = ((size_t)blockIdx.y * a.G + (tid & (a.G - 1))) * W;
-    const bool mine = c < a.D;
-    const bool note = blockIdx.y == 0 && (tid & (a.G - 1)) == 0;
-    if (note) a.begins[share] = inside ? j : NO_ROW;
-
-    float acc[W];
-#pragma unroll
-    for (int x = 0; x < W; ++x) acc[x] = 0.0f;
-    bool open = inside, first = inside;                              // the row has tokens; it began in an earlier share
-    auto row_end = [&]() {
-        if (first) {
-            if (mine) store_vec<float, W>(a.head + (size_t)share * a.D + c, acc);
-            if (note) {
-                const uint32_t k = atomicAdd(a.joins, 1u);           // (the list's order does not matter: every row joins for itself)
-                a.joins[1 + 2 * k] = share;
-                a.joins[2 + 2 * k] = j;
-            }
-        } else if (mine && (open || !a.accumulate)) {
-            write_row<TO, W>(grad + (size_t)j * a.out_stride + c, acc, a.scale, a.accumulate != 0);
+    // the group's share of the tokens; borders inside a row move as the block's do
+    const uint32_t g = tid / a.G, member = tid & (a.G - 1);
+    auto inner = [&](uint32_t i) {
+        if (i == 0 || i >= n || s_key[i] != s_key[i + 1]) return i;
+        uint32_t f = i > GR_LONG ? i - GR_LONG : 0, hi = i;
+        const uint32_t k = s_key[i];
+        while (f < hi) {                                             // the row's first token in the block, looking back GR_LONG tokens
+            const uint32_t m = (f + hi) / 2;
+            if (s_key[m + 1] < k) f = m + 1; else hi = m;
         }
-        ++j;
-        open = first = false;
+        return i - f < GR_LONG && s_key[f] != k ? f : i;             // (s_key[f] == k: it began before the block, behind a border that cuts it)
+    };
+    const uint32_t each = (n + groups - 1) / groups;
+    uint32_t i = inner(g * each < n ? g * each : n);
+    const uint32_t i_end = inner((g + 1) * each < n ? (g + 1) * each : n);
+    const uint32_t share = blockIdx.x * groups + g;
+    uint32_t row = s_key[i];                                         // the current row: it goes on from the share before, or there is none yet
+    const bool inside = row < a.V && row == s_key[i + 1];
+    const bool note = blockIdx.y == 0 && member == 0;
+    if (note) a.begins[share] = inside ? row : NO_ROW;
+
+    const size_t c0 = ((size_t)blockIdx.y * a.G * NU + member) * U;  // unit u: columns c0 + u G U ...
+    const size_t cstep = (size_t)a.G * U;
+    bool mine[NU];
 #pragma unroll
-        for (int x = 0; x < W; ++x) acc[x] = 0.0f;
+    for (int u = 0; u < NU; ++u) mine[u] = c0 + u * cstep < a.D;
+    constexpr int FLY = GR_INFLIGHT / (NU > 2 ? 2 : 1);
+    raw_vec<TI, U> v[FLY][NU];
+    uint32_t key[FLY];
+    auto fetch = [&] {                                               // (no branch around a load: it would be waited for in it)
+        const TI* src[FLY];
+#pragma unroll
+        for (int q = 0; q < FLY; ++q) {
+            const uint32_t at = i + q < i_end ? i + q : i;
+            key[q] = s_key[at + 1];
+            src[q] = dout + (size_t)s_pos[at] * a.in_stride + c0;    // (a token that gives nothing has a position as well)
+        }
+#pragma unroll
+        for (int q = 0; q < FLY; ++q)
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+                if (i + q < i_end && mine[u]) v[q][u] = load_raw<TI, U>(src[q] + u * cstep);
+    };
+    if (i < i_end) fetch();
+    if (!a.accumulate) {                                             // zeros, while the first rows are on their way
+        const size_t first = (size_t)blockIdx.y * a.G * NU * U, width = (size_t)a.G * NU * U;
+        const uint32_t cols = (uint32_t)(a.D - first < width ? a.D - first : width), rows = row1 - row0;
+        const bool dense = cols == a.D && a.out_stride == a.D;       // rows follow each other without gaps
+        const uint32_t hi = rows * (w + 1) / (GR_THREADS / 32);
+        for (uint32_t r = rows * w / (GR_THREADS / 32); r < hi;) {   // the warp's rows: runs [r, e) without tokens
+            const uint32_t none = ~s_has[r >> 5] >> (r & 31);
+            if (none == 0) { r = (r | 31) + 1; continue; }
+            r += __ffs(none) - 1;
+            uint32_t e = r;
+            while (e < hi) {
+                const uint32_t some = s_has[e >> 5] >> (e & 31);
+                if (some != 0) { e += __ffs(some) - 1; break; }
+                e = (e | 31) + 1;
+            }
+            if (e > hi) e = hi;
+            TO* p = grad + (size_t)(row0 + r) * a.out_stride + first;
+            if (dense) {
+                if (r < e) zero_span(p, (size_t)(e - r) * cols, lane);
+            } else {
+                for (uint32_t q = r; q < e; ++q, p += a.out_stride) zero_span(p, cols, lane);
+            }
+            r = e;
+        }
+    }
+    float acc[NU][U];
+    auto clear = [&] {
+#pragma unroll
+        for (int u = 0; u < NU; ++u)
+#pragma unroll
+            for (int x = 0; x < U; ++x) acc[u][x] = 0.0f;
+    };
+    clear();
+    bool open = inside, first = inside;                              // there is a current row; it began in an earlier share
+    auto close = [&] {
+        if (first) {
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+                if (mine[u]) store_vec<float, U>(a.head + (size_t)share * a.D + c0 + u * cstep, acc[u]);
+            if (note) {
+                const uint32_t q = atomicAdd(a.joins, 1u);           // (the list's order does not matter: every row joins for itself)
+                a.joins[1 + 2 * q] = share;
+                a.joins[2 + 2 * q] = row;
+            }
+        } else {
+            TO* out = grad + (size_t)row * a.out_stride + c0;
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+                if (mine[u]) write_unit<TO, U>(out + u * cstep, acc[u], a.scale, a.accumulate != 0);
+        }
+        first = false;
+        clear();
     };
     while (i < i_end) {
-        raw_vec<TI, W> v[GR_INFLIGHT];
-        const int cnt = i_end - i < GR_INFLIGHT ? (int)(i_end - i) : GR_INFLIGHT;
 #pragma unroll
-        for (int q = 0; q < GR_INFLIGHT; ++q)
-            if (q < cnt && mine && s_key[i + q + 1] < a.V) v[q] = load_raw<TI, W>(dout + (size_t)s_pos[i + q] * a.in_stride + c);
+        for (int q = 0; q < FLY; ++q) {
+            if (i + q < i_end) {
+                const uint32_t k = key[q];
+                if (k != row || !open) {
+                    if (open) close();
+                    row = k;
+                    open = k < a.V;
+                }
+                if (open) {
 #pragma unroll
-        for (int q = 0; q < GR_INFLIGHT; ++q) {
-            if (q < cnt) {
-                const uint32_t k = s_key[i + q + 1];
-                while (j < k) row_end();
-                if (k < a.V) {
-                    open = true;
-                    if (mine) {
-                        float x[W];
-                        unpack<TI, W>(v[q], x);
+                    for (int u = 0; u < NU; ++u)
+                        if (mine[u]) {
+                            float x[U];
+                            unpack<TI, U>(v[q][u], x);
 #pragma unroll
-                        for (int z = 0; z < W; ++z) acc[z] += x[z];
-                    }
+                            for (int z = 0; z < U; ++z) acc[u][z] += x[z];
+                        }
                 }
             }
         }
-        i += cnt;
+        i += FLY;
+        if (i < i_end) fetch();
     }
-    while (j < j_end) row_end();
-    if (open && mine) store_vec<float, W>(a.tail + (size_t)share * a.D + c, acc);
+    if (open) {
+        if (s_key[i_end + 1] != row) {
+            close();
+        } else {
+#pragma unroll
+            for (int u = 0; u < NU; ++u)
+                if (mine[u]) store_vec<float, U>(a.tail + (size_t)share * a.D + c0 + u * cstep, acc[u]);
+        }
+    }
 }
 
 // ---- joining the rows that cross shares --------------------------------------------------------------------------
@@ -422,7 +666,7 @@ __global__ void __launch_bounds__(JN_THREADS) grad_join_kernel(const GradArgs a,
                 float sum[1] = {0.0f};
                 for (int q = 0; q < JN_WARPS; ++q) sum[0] += s_part[q][threadIdx.x];
                 sum[0] += a.head[(size_t)s * a.D + c];
-                write_row<TO, 1>(grad + (size_t)j * a.out_stride + c, sum, a.scale, a.accumulate != 0);
+                write_unit<TO, 1>(grad + (size_t)j * a.out_stride + c, sum, a.scale, a.accumulate != 0);
             }
             __syncthreads();
         }
@@ -436,7 +680,7 @@ struct GradLayout {
     uint32_t tiles;
     int passes, bits;
 };
-// The widest plan of the two (vector or element-wise rows) sizes the workspace.
+// Sized for either input type (4 or 8 elements of a row a thread).
 void grad_layout(size_t T, size_t V, size_t D, GradLayout* L) {
     size_t off = 0;
     L->tiles = (uint32_t)((T + SORT_TILE - 1) / SORT_TILE);
@@ -451,10 +695,9 @@ void grad_layout(size_t T, size_t V, size_t D, GradLayout* L) {
     L->hist = off; off = align_up(off + (size_t)SORT_BINS * L->tiles * 4, 256);
     L->totals = off; off = align_up(off + SORT_BINS * 4, 256);
     size_t shares = 0;
-    const int widths[3] = {1, 4, 8};
-    for (int q = 0; q < 3; ++q) {
-        const size_t s = grad_plan(T, V, D, widths[q]).shares;
-        shares = s > shares ? s : shares;
+    for (int W = 4; W <= 8; W += 4) {
+        const size_t n = grad_plan(T, V, D, 1, W).shares;
+        shares = n > shares ? n : shares;
     }
     L->joins = off; off = align_up(off + (1 + 2 * shares) * 4, 256);
     L->begins = off; off = align_up(off + shares * 4, 256);
@@ -466,6 +709,21 @@ void grad_layout(size_t T, size_t V, size_t D, GradLayout* L) {
 template <class IDX>
 int sort_tokens(SortArgs a, const GradLayout& L, char* ws, cudaStream_t st) {
     a.bins = 1 << L.bits;
+    if (a.T <= 8u * CS_THREADS * CS_MAX_ITEMS) {
+        ClusterSortArgs c = {};
+        c.tokens = a.tokens; c.joins = a.joins;
+        c.keys = reinterpret_cast<uint32_t*>(ws + L.keys[(L.passes - 1) & 1]);
+        c.pos = reinterpret_cast<uint32_t*>(ws + L.pos[(L.passes - 1) & 1]);
+        c.T = a.T; c.V = a.V; c.skip = a.skip; c.bits = L.bits; c.passes = L.passes;
+        unsigned blocks = 1;                                       // few items a thread first, then more blocks
+        while (blocks < 8 && a.T > blocks * CS_THREADS) blocks *= 2;
+        const unsigned per = (a.T + blocks * CS_THREADS - 1) / (blocks * CS_THREADS);
+        if (per <= 1) return launch_cluster_sort<IDX, 1>(c, blocks, st);
+        if (per <= 2) return launch_cluster_sort<IDX, 2>(c, blocks, st);
+        if (per <= 4) return launch_cluster_sort<IDX, 4>(c, blocks, st);
+        if (per <= 8) return launch_cluster_sort<IDX, 8>(c, blocks, st);
+        return launch_cluster_sort<IDX, 16>(c, blocks, st);
+    }
     for (int pass = 0; pass < L.passes; ++pass) {
         a.shift = pass * L.bits;
         const int src = (pass + 1) & 1, dst = pass & 1;
@@ -482,8 +740,10 @@ int sort_tokens(SortArgs a, const GradLayout& L, char* ws, cudaStream_t st) {
     return EC_OK;
 }
 
-template <class TI, class TO, int W>
-int launch_walk(GradArgs a, const GradPlan& p, const void* dout, void* grad, cudaStream_t st) {
+template <class TI, class TO, int U>
+int launch_walk(GradArgs a, const void* dout, void* grad, cudaStream_t st) {
+    constexpr int W = sizeof(TI) == 2 ? 8 : 4;
+    const GradPlan p = grad_plan(a.T, a.V, a.D, U, W);
     a.G = p.G;
     a.C = p.C;
     cudaLaunchConfig_t cfg = {};
@@ -492,7 +752,8 @@ int launch_walk(GradArgs a, const GradPlan& p, const void* dout, void* grad, cud
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = st;
     cfg.gridDim = dim3(p.blocks, p.slices); cfg.blockDim = dim3(GR_THREADS);
-    EC_CUDA(cudaLaunchKernelEx(&cfg, grad_walk_kernel<TI, TO, W>, a, static_cast<const TI*>(dout), static_cast<TO*>(grad)));
+    EC_CUDA(cudaLaunchKernelEx(&cfg, grad_walk_kernel<TI, TO, U, W / U>, a, static_cast<const TI*>(dout), static_cast<TO*>(grad)));
+    if (a.T <= GR_LONG) return EC_OK;                  // no row is long enough to be cut
     const size_t cols = (a.D + 127) / 128;
     cfg.gridDim = dim3(p.shares < 148 ? p.shares : 148, (unsigned)(cols < 16 ? cols : 16)); cfg.blockDim = dim3(JN_THREADS);
     EC_CUDA(cudaLaunchKernelEx(&cfg, grad_join_kernel<TO>, a, static_cast<TO*>(grad)));
@@ -568,10 +829,13 @@ int ec_embed_grad(const void* dout, size_t dout_stride, ec_dtype_t dout_dtype, c
     }
     return with_types(dout_dtype, grad_dtype, [&](auto ti, auto to) {
         using TI = decltype(ti); using TO = decltype(to);
-        constexpr int W = sizeof(TI) == 2 ? 8 : 4;
-        const bool vec = D % W == 0 && rows_aligned(dout, dout_stride, sizeof(TI), W) && rows_aligned(grad, grad_stride, sizeof(TO), W);
-        if (vec) return launch_walk<TI, TO, W>(a, grad_plan(T, V, D, W), dout, grad, stream);
-        return launch_walk<TI, TO, 1>(a, grad_plan(T, V, D, 1), dout, grad, stream);
+        const int u = unit_of<TI, TO>(D, dout, dout_stride, grad, grad_stride);
+        if constexpr (sizeof(TI) == 2) {
+            if (u == 8) return launch_walk<TI, TO, 8>(a, dout, grad, stream);
+        }
+        if (u == 4) return launch_walk<TI, TO, 4>(a, dout, grad, stream);
+        if (u == 2) return launch_walk<TI, TO, 2>(a, dout, grad, stream);
+        return launch_walk<TI, TO, 1>(a, dout, grad, stream);
     });
 }
 

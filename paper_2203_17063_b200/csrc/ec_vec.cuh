@@ -78,9 +78,11 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[W]) {   // writ
 #pragma unroll
             for (int i = 0; i < W / 4; ++i)
                 __stcs(reinterpret_cast<float4*>(p) + i, make_float4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]));
+        } else if constexpr (W == 2) {
+            __stcs(reinterpret_cast<float2*>(p), make_float2(x[0], x[1]));
         } else {
-#pragma unroll
-            for (int i = 0; i < W; ++i) __stcs(reinterpret_cast<float*>(p) + i, x[i]);
+            static_assert(W == 1, "one, two or a multiple of four");
+            __stcs(reinterpret_cast<float*>(p), x[0]);
         }
     } else {
         if constexpr (W == 8) {
@@ -88,14 +90,16 @@ __device__ __forceinline__ void store_vec(T* p, const float (&x)[W]) {   // writ
                                                            pack2_bf16(x[4], x[5]), pack2_bf16(x[6], x[7])));
         } else if constexpr (W == 4) {
             __stcs(reinterpret_cast<uint2*>(p), make_uint2(pack2_bf16(x[0], x[1]), pack2_bf16(x[2], x[3])));
+        } else if constexpr (W == 2) {
+            __stcs(reinterpret_cast<unsigned int*>(p), pack2_bf16(x[0], x[1]));
         } else {
-            static_assert(W == 1, "one, four or eight bf16");
+            static_assert(W == 1, "one, two, four or eight bf16");
             __stcs(reinterpret_cast<unsigned short*>(p), (unsigned short)(pack2_bf16(x[0], 0.0f) & 0xffffu));
         }
     }
 }
 
-// Can rows of `stride` elements of `size` bytes from `base` be read or written W elements at a time?
+// Can rows of `stride` elements of `size` bytes from `base` be read or written in units of W elements (of 16 bytes at most)?
 inline bool rows_aligned(const void* base, size_t stride, size_t size, int W) {
     const size_t a = size * (size_t)W < 16 ? size * (size_t)W : 16;
     return reinterpret_cast<uintptr_t>(base) % a == 0 && stride * size % a == 0;
