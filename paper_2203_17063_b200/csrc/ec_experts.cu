@@ -29,10 +29,11 @@ struct ExpertArgs {
     int E, N, K, accumulate;
 };
 
-// The row ranges of the experts in shared memory, and the number of row tiles of `tile` rows before each expert.  All threads
-// of the block; returns false (and block 0 says so in *status) if displs does not ascend within [0, T].
+// The row ranges of the experts in shared memory, and the number of row tiles of `tile` rows before each expert (`plus` more
+// for every expert).  All threads of the block; returns false (and block 0 says so in *status) if displs does not ascend
+// within [0, T].
 template <int THREADS>
-__device__ bool expert_ranges(const ExpertArgs& a, int tile, int* s_row, int* s_tile, int* s_warp) {
+__device__ bool expert_ranges(const ExpertArgs& a, int tile, int plus, int* s_row, int* s_tile, int* s_warp) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     bool ok = true;
     int carry = 0;
@@ -46,7 +47,7 @@ __device__ bool expert_ranges(const ExpertArgs& a, int tile, int* s_row, int* s_
             } else {
                 s_row[e] = (int)b;
                 if (e == a.E - 1) s_row[a.E] = (int)d;
-                n = (int)((d - b + tile - 1) / tile);
+                n = (int)((d - b + tile - 1) / tile) + plus;
             }
         }
         int inc = n;
@@ -90,7 +91,7 @@ template <class TI, class TO, int MODE>
 __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertArgs a) {
     __shared__ int s_row[MAX_EXPERTS + 1], s_tile[MAX_EXPERTS + 1], s_warp[SC_THREADS / 32];
     __shared__ float s_a[SC_STEP][SC_TILE + 4], s_b[SC_STEP][SC_TILE + 4];
-    if (!expert_ranges<SC_THREADS>(a, SC_TILE, s_row, s_tile, s_warp)) return;
+    if (!expert_ranges<SC_THREADS>(a, SC_TILE, 0, s_row, s_tile, s_warp)) return;
     const int rows_out = MODE == EX_WEIGHT ? a.N : 0, cols_out = MODE == EX_FORWARD ? a.N : a.K;
     const int jt = (cols_out + SC_TILE - 1) / SC_TILE, it = (rows_out + SC_TILE - 1) / SC_TILE;
     const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * it * jt : (long long)s_tile[a.E] * jt;
@@ -163,25 +164,32 @@ __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertA
 }
 
 // ---- products on the tensor cores --------------------------------------------------------------------------------
-// One persistent block per SM, 128 x bn tiles of the result, reduction in steps of 64:
-//   producer (one thread)  brings the two operand tiles of a step into a ring of shared-memory stages by bulk tensor copies.
-//                          Rows of another expert that a copy brings along only reach result rows that are not stored; where
-//                          rows are the reduction (weight grad) the last step's foreign rows are overwritten with zeros
-//                          before the product, both operands, since they may hold infinities or NaN;
-//   issuer (one warp)      multiplies a landed stage, as it lies, into one of two accumulators in tensor memory;
+// Persistent blocks, one per SM, or pairs of blocks (PAIR) that share a tile: 128 rows of the result a block, bn columns,
+// reduction in steps of 64:
+//   producer (one thread)  brings the block's operand tiles of a step into a ring of shared-memory stages by bulk tensor
+//                          copies.  Rows of another expert that a copy brings along only reach result rows that are not stored;
+//                          where rows are the reduction (weight grad) the last step's foreign rows are overwritten with
+//                          zeros before the product, both operands, since they may hold infinities or NaN;
+//   issuer (one thread, of a pair's first block)  multiplies a landed stage, as it lies, into one of two accumulators in tensor memory;
 //   epilogue (four warps)  reads the finished accumulator while the next tile's products run, rounds once and writes it out
 //                          through a small transposing buffer, so that a warp's stores cover whole 128-byte lines.
+// A pair multiplies 256 x bn: each block brings its 128 rows of A and half of B's columns, and the tensor cores read the other
+// half of B from the other block.  A block alone needs 16 + 32 KB of operands, written and read, for the 512 cycles of a step at
+// bn = 256 - 190 bytes a cycle of shared memory's 128, and a step took 768 cycles (K-major) to 1100 (MN-major) by clock64; in a
+// pair it is 16 + 16 KB.
 // Operands: x and dy are K-major where their columns are the reduction, MN-major in the weight grad; W is K-major in the
 // forward and MN-major in the input grad: no operand is transposed in memory.
 // Every wait is bounded; a wait that gives up raises a flag that all roles poll, the block sets *status to 2, waits for its
 // copies in flight, frees its tensor memory and returns.
 
-constexpr int MM_THREADS = 256, MM_ROWS = 128, MM_STEP = 64, MM_MAX_STAGES = 8;
+constexpr int MM_THREADS = 256, MM_ROWS = 128, MM_STEP = 64, MM_MAX_STAGES = 12;
 constexpr int MM_PITCH = 144;                                  // bytes of a 128-byte row in the transposing buffer
+constexpr int MM_TILE_COST = 3;                                // writing a tile out, in reduction steps (for sharing out the weight grad)
+constexpr uint32_t MM_SMEM = 200 * 1024;                       // dynamic shared memory, beside 27 KB of static
 
 struct MmaPlan {
-    int bm, bn, stages;                                        // rows a tile takes (<= 128), columns, ring stages
-    uint32_t a_bytes, b_bytes, stage_bytes, tx_bytes, tmem_cols, idesc, smem;
+    int bm, bn, stages;                                        // rows of A a block takes (<= 128), columns of the tile, ring stages
+    uint32_t a_bytes, b_bytes, stage_bytes, tmem_cols, idesc, smem;
 };
 
 // One warp writes its 32 rows (`height` of them exist) of a finished tile, `width` columns from tensor-memory column src on
@@ -238,55 +246,80 @@ __device__ __forceinline__ void store_tile(TO* out, size_t stride, int height, i
     }
 }
 
-template <class TO, int MODE>
+template <class TO, int MODE, bool PAIR>
 __global__ void __launch_bounds__(MM_THREADS, 1)
 expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ExpertArgs a, const MmaPlan pl) {
     using namespace mma;
     extern __shared__ unsigned char mm_raw[];
     __shared__ int s_row[MAX_EXPERTS + 1], s_tile[MAX_EXPERTS + 1], s_warp[MM_THREADS / 32];
-    __shared__ __align__(8) uint64_t s_bar[2 * MM_MAX_STAGES + 4];
+    __shared__ __align__(8) uint64_t s_bar[3 * MM_MAX_STAGES + 4];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
     __shared__ __align__(16) unsigned char s_out[4][32 * MM_PITCH];
+    constexpr int BLOCKS = PAIR ? 2 : 1;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    if (!expert_ranges<MM_THREADS>(a, pl.bm, s_row, s_tile, s_warp)) return;
+    const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u;
+    const uint32_t worker = blockIdx.x / BLOCKS, workers = gridDim.x / BLOCKS;
+    const int tile_rows = pl.bm * BLOCKS;                      // rows of a tile
+    if (!expert_ranges<MM_THREADS>(a, MODE == EX_WEIGHT ? MM_STEP : tile_rows, MODE == EX_WEIGHT ? MM_TILE_COST : 0, s_row, s_tile, s_warp)) return;
 
     unsigned char* sm = mm_raw + ((1024u - (smem_u32(mm_raw) & 1023u)) & 1023u);
-    const uint32_t stage0 = smem_u32(sm), bar0 = smem_u32(s_bar);
-    auto B_full = [&](int s) { return bar0 + 8u * (uint32_t)s; };
-    auto B_empty = [&](int s) { return bar0 + 8u * (uint32_t)(MM_MAX_STAGES + s); };
-    auto B_accfull = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MM_MAX_STAGES + b); };
-    auto B_accempty = [&](int b) { return bar0 + 8u * (uint32_t)(2 * MM_MAX_STAGES + 2 + b); };
+    const uint32_t stage0 = smem_u32(sm), bar0 = smem_u32(s_bar), nst = (uint32_t)pl.stages;
+    auto B_full = [&](uint32_t s) { return bar0 + 8u * s; };                               // used: the first block's
+    auto B_empty = [&](uint32_t s) { return bar0 + 8u * (MM_MAX_STAGES + s); };
+    auto B_tail = [&](uint32_t s) { return bar0 + 8u * (2 * MM_MAX_STAGES + s); };
+    auto B_accfull = [&](uint32_t b) { return bar0 + 8u * (3 * MM_MAX_STAGES + b); };
+    auto B_accempty = [&](uint32_t b) { return bar0 + 8u * (3 * MM_MAX_STAGES + 2 + b); }; // used: the first block's
     if (tid == 0) {
-        for (int s = 0; s < pl.stages; ++s) { mbar_init(B_full(s), 1); mbar_init(B_empty(s), 1); }
-        for (int b = 0; b < 2; ++b) { mbar_init(B_accfull(b), 1); mbar_init(B_accempty(b), 4); }
+        for (uint32_t s = 0; s < nst; ++s) { mbar_init(B_full(s), BLOCKS); mbar_init(B_empty(s), 1); mbar_init(B_tail(s), 1); }
+        for (uint32_t b = 0; b < 2; ++b) { mbar_init(B_accfull(b), 1); mbar_init(B_accempty(b), 4 * BLOCKS); }
         s_abort = 0;
         mbar_init_fence();
     }
-    if (warp == 2) tmem_alloc(smem_u32(&s_tmem), pl.tmem_cols);
+    if (warp == 2) tmem_alloc<PAIR>(smem_u32(&s_tmem), pl.tmem_cols);
     fence_before_sync();
     __syncthreads();
+    if (PAIR) cluster_sync();                                  // both blocks' barriers stand
     fence_after_sync();
     const uint32_t tmem = s_tmem;
 
     // the tiles: for each expert, down the rows first
     const int cols = MODE == EX_FORWARD ? a.N : a.K, jt = (cols + pl.bn - 1) / pl.bn;
-    const int wt = (a.N + MM_ROWS - 1) / MM_ROWS;
-    const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * wt * jt : (long long)s_tile[a.E] * jt;
-    struct Tile { int e, i, i_end, j, len; };                  // expert, first result row, end of its rows, first column, reduction length
+    const int wt = (a.N + MM_ROWS * BLOCKS - 1) / (MM_ROWS * BLOCKS);
+    long long t0 = worker, t1, dt = workers;
+    if (MODE == EX_WEIGHT) {
+        // Tiles of one expert cost the same, those of another expert more or less: every worker takes a run of tiles of about
+        // the same cost.  s_tile[e] = cost of one tile of each expert before e.
+        const long long per = (long long)wt * jt, all = per * s_tile[a.E];
+        auto first_from = [&](long long cost) {                // first tile that begins at `cost` or later
+            int lo = 0, hi = a.E - 1;
+            while (lo < hi) {
+                const int m = (lo + hi + 1) / 2;
+                if (per * s_tile[m] <= cost) lo = m; else hi = m - 1;
+            }
+            const long long c = s_tile[lo + 1] - s_tile[lo], q = (cost - per * s_tile[lo] + c - 1) / c;
+            return lo * per + (q < per ? q : per);
+        };
+        t0 = first_from(all * worker / workers);
+        t1 = first_from(all * (worker + 1) / workers);
+        dt = 1;
+    } else {
+        t1 = (long long)s_tile[a.E] * jt;
+    }
+    struct Tile { int e, i, i_end, j, len; };                  // expert, the block's first result row, end of its rows, first column, reduction length
     auto tile_of = [&](long long t) {
         Tile x;
         if (MODE == EX_WEIGHT) {
             x.e = (int)(t / ((long long)wt * jt));
             const int q = (int)(t - (long long)x.e * wt * jt);
-            x.i = (q % wt) * MM_ROWS;
-            x.i_end = a.N;
+            x.i = (q % wt) * (MM_ROWS * BLOCKS) + (int)rank * MM_ROWS;
+            x.i_end = x.i + MM_ROWS < a.N ? x.i + MM_ROWS : a.N;
             x.j = (q / wt) * pl.bn;
             x.len = s_row[x.e + 1] - s_row[x.e];
         } else {
             x.e = expert_of(s_tile, a.E, (int)(t / jt));
             const int mt = s_tile[x.e + 1] - s_tile[x.e], q = (int)(t - (long long)s_tile[x.e] * jt);
-            x.i = s_row[x.e] + (q % mt) * pl.bm;
+            x.i = s_row[x.e] + (q % mt) * tile_rows + (int)rank * pl.bm;
             x.i_end = x.i + pl.bm < s_row[x.e + 1] ? x.i + pl.bm : s_row[x.e + 1];
             x.j = (q / mt) * pl.bn;
             x.len = MODE == EX_FORWARD ? a.K : a.N;
@@ -295,105 +328,124 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     };
 
     bool ok = true;
-    uint32_t filled = 0;                                       // stages the producer has filled
-    if (warp == 0) {
-        if (lane == 0) {
-            for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
-                const Tile x = tile_of(t);
-                for (int l = 0; l < x.len; l += MM_STEP) {
-                    const int s = (int)(filled % (uint32_t)pl.stages);
-                    const uint32_t use = filled / (uint32_t)pl.stages;
-                    if (use > 0 && !wait_or_abort(B_empty(s), (use - 1) & 1u, &s_abort)) { ok = false; break; }
-                    const uint32_t sa = stage0 + (uint32_t)s * pl.stage_bytes, sb = sa + pl.a_bytes;
-                    mbar_expect_tx(B_full(s), pl.tx_bytes);
-                    if (MODE == EX_WEIGHT) {
-                        const int r = s_row[x.e] + l;
-                        for (int q = 0; q < MM_ROWS / 64; ++q) tma_load_2d(sa + q * 8192u, &map_a, x.i + 64 * q, r, B_full(s));
-                        for (int q = 0; q < pl.bn / 64; ++q) tma_load_2d(sb + q * 8192u, &map_b, x.j + 64 * q, r, B_full(s));
-                    } else {
-                        tma_load_2d(sa, &map_a, l, x.i, B_full(s));
-                        if (MODE == EX_FORWARD) tma_load_3d(sb, &map_b, l, x.j, x.e, B_full(s));
-                        else for (int q = 0; q < pl.bn / 64; ++q) tma_load_3d(sb + q * 8192u, &map_b, x.j + 64 * q, l, x.e, B_full(s));
-                    }
-                    ++filled;
-                }
-            }
-            if (s_abort != 0)                                  // copies in flight land before the block may go
-                for (uint32_t f = filled > (uint32_t)pl.stages ? filled - pl.stages : 0; f < filled; ++f)
-                    for (uint32_t it = 0; it < (1u << 12); ++it)
-                        if (mbar_try_wait(B_full((int)(f % (uint32_t)pl.stages)), (f / (uint32_t)pl.stages) & 1u)) break;
-        }
-    } else if (warp == 1) {
-        uint32_t n = 0, acc = 0;                               // stages multiplied, accumulators filled
-        for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+    const uint32_t bar_first = PAIR ? peer_address(bar0, 0) : bar0;             // the barriers of the pair's first block
+    if (warp == 0 && lane == 0) {
+        const int bh = pl.bn / BLOCKS;                         // columns of B the block brings
+        uint32_t s = 0, use = 0;                               // the next stage, times the ring has been filled
+        for (long long t = t0; t < t1 && ok; t += dt) {
             const Tile x = tile_of(t);
-            if (x.len == 0) continue;
-            const int buf = (int)(acc & 1u);
-            if (acc >= 2) ok = __all_sync(0xffffffffu, wait_or_abort(B_accempty(buf), ((acc >> 1) - 1) & 1u, &s_abort));   // (the warp goes on, or leaves, together)
-            if (!ok) break;
-            fence_after_sync();
+            const int jb = x.j + (int)rank * bh;
             for (int l = 0; l < x.len; l += MM_STEP) {
-                const int s = (int)(n % (uint32_t)pl.stages);
-                ok = __all_sync(0xffffffffu, wait_or_abort(B_full(s), (n / (uint32_t)pl.stages) & 1u, &s_abort));
-                if (!ok) break;
-                fence_after_sync();
-                const uint32_t sa = stage0 + (uint32_t)s * pl.stage_bytes, sb = sa + pl.a_bytes;
-                if (MODE == EX_WEIGHT && x.len - l < MM_STEP) {
-                    const int keep = x.len - l, boxes = (MM_ROWS + pl.bn) / 64, items = (MM_STEP - keep) * 8;
-                    for (int q = lane; q < boxes * items; q += 32) {
-                        const int box = q / items, p = q - box * items;
-                        *reinterpret_cast<uint4*>(sm + (size_t)s * pl.stage_bytes + box * 8192 + keep * 128 + p * 16) = make_uint4(0, 0, 0, 0);
-                    }
-                    fence_async_smem();
-                    __syncwarp();
+                if (use > 0 && !wait_or_abort(B_empty(s), (use - 1) & 1u, &s_abort)) { ok = false; break; }
+                const uint32_t sa = stage0 + s * pl.stage_bytes, sb = sa + pl.a_bytes;
+                const bool tail = MODE == EX_WEIGHT && x.len - l < MM_STEP;                // its landing is seen by the block's own tail warp first
+                const uint32_t bar = tail ? B_tail(s) : bar_first + 8u * s;
+                if (tail || !PAIR || rank == 0) mbar_expect_tx(tail ? bar : B_full(s), pl.stage_bytes);
+                else mbar_expect_tx_peer(bar, pl.stage_bytes);
+                if (MODE == EX_WEIGHT) {
+                    const int r = s_row[x.e] + l;
+                    for (int q = 0; q < MM_ROWS / 64; ++q) tma_load_2d<PAIR>(sa + q * 8192u, &map_a, x.i + 64 * q, r, bar);
+                    for (int q = 0; q < bh / 64; ++q) tma_load_2d<PAIR>(sb + q * 8192u, &map_b, jb + 64 * q, r, bar);
+                } else {
+                    tma_load_2d<PAIR>(sa, &map_a, l, x.i, bar);
+                    if (MODE == EX_FORWARD) tma_load_3d<PAIR>(sb, &map_b, l, jb, x.e, bar);
+                    else for (int q = 0; q < bh / 64; ++q) tma_load_3d<PAIR>(sb + q * 8192u, &map_b, jb + 64 * q, l, x.e, bar);
                 }
-                if (lane == 0) {
-#pragma unroll
-                    for (int k = 0; k < MM_STEP / 16; ++k) {
-                        const uint64_t da = operand_desc(sa + k * (MODE == EX_WEIGHT ? 2048u : 32u), MODE == EX_WEIGHT ? 8192u : 16u);
-                        const uint64_t db = operand_desc(sb + k * (MODE == EX_FORWARD ? 32u : 2048u), MODE == EX_FORWARD ? 16u : 8192u);
-                        mma_bf16(tmem + (uint32_t)(buf * pl.bn), da, db, pl.idesc, l > 0 || k > 0 ? 1u : 0u);
-                    }
-                    mma_commit(B_empty(s));
-                    if (l + MM_STEP >= x.len) mma_commit(B_accfull(buf));
-                }
-                __syncwarp();
-                ++n;
+                if (++s == nst) { s = 0; ++use; }
             }
+        }
+        // Copies in flight land before the block may go: after the last tile the products have waited for them; after a wait that
+        // gave up, a bounded time is given.
+        if (s_abort != 0) {
+            const long long c0 = clock64();
+            while (clock64() - c0 < 20000000LL) {}
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // One thread issues everything: with a warp waiting together and ring positions by division a step took it 890 cycles, the
+        // products themselves 512.
+        const uint64_t base_a = operand_desc(0, MODE == EX_WEIGHT ? 8192u : 16u), base_b = operand_desc(0, MODE == EX_FORWARD ? 16u : 8192u);
+        constexpr uint32_t STEP_A = (MODE == EX_WEIGHT ? 2048u : 32u) >> 4, STEP_B = (MODE == EX_FORWARD ? 32u : 2048u) >> 4;
+        uint32_t s = 0, phase = 0, acc = 0;                    // the next stage and its parity, accumulators filled
+        for (long long t = t0; t < t1 && ok; t += dt) {
+            const int len = tile_of(t).len;
+            if (len == 0) continue;
+            const uint32_t buf = acc & 1u, d = tmem + buf * (uint32_t)pl.bn;
+            if (acc >= 2 && !wait_or_abort(B_accempty(buf), ((acc >> 1) - 1) & 1u, &s_abort)) break;
+            fence_after_sync();
+            for (int l = 0; l < len; l += MM_STEP) {
+                if (!wait_or_abort(B_full(s), phase, &s_abort)) { ok = false; break; }
+                fence_after_sync();
+                const uint32_t sa = stage0 + s * pl.stage_bytes;
+                const uint64_t da = base_a + (sa >> 4), db = base_b + ((sa + pl.a_bytes) >> 4);
+#pragma unroll
+                for (uint32_t k = 0; k < MM_STEP / 16; ++k) mma_bf16<PAIR>(d, da + k * STEP_A, db + k * STEP_B, pl.idesc, l > 0 || k > 0 ? 1u : 0u);
+                mma_commit<PAIR>(B_empty(s));
+                if (++s == nst) { s = 0; phase ^= 1u; }
+            }
+            if (ok) mma_commit<PAIR>(B_accfull(buf));
             ++acc;
+        }
+    } else if (MODE == EX_WEIGHT && warp == 3) {
+        // the last step's rows of the next expert: zeros in both operands
+        uint32_t s = 0, tails = 0;                             // the next stage, parity of each stage's tail barrier
+        for (long long t = t0; t < t1 && ok; t += dt) {
+            const int len = tile_of(t).len, keep = len % MM_STEP;
+            s = (s + (uint32_t)(len / MM_STEP)) % nst;
+            if (keep == 0) continue;
+            ok = __all_sync(0xffffffffu, wait_or_abort(B_tail(s), (tails >> s) & 1u, &s_abort));       // (the warp goes on, or leaves, together)
+            if (!ok) break;
+            tails ^= 1u << s;
+            const int boxes = (int)(pl.stage_bytes / 8192u), items = (MM_STEP - keep) * 8;
+            for (int q = lane; q < boxes * items; q += 32) {
+                const int box = q / items, p = q - box * items;
+                *reinterpret_cast<uint4*>(sm + (size_t)s * pl.stage_bytes + box * 8192 + keep * 128 + p * 16) = make_uint4(0, 0, 0, 0);
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+                if (rank == 0) mbar_arrive(B_full(s));
+                else mbar_arrive_peer(bar_first + 8u * s);
+            }
+            if (++s == nst) s = 0;
         }
     } else if (warp >= 4) {
         const int w = warp - 4;
         uint32_t acc = 0;
-        for (long long t = blockIdx.x; t < tiles && ok; t += gridDim.x) {
+        for (long long t = t0; t < t1 && ok; t += dt) {
             const Tile x = tile_of(t);
             if (MODE == EX_WEIGHT && x.len == 0 && a.accumulate) continue;
-            const int buf = (int)(acc & 1u);
+            const uint32_t buf = acc & 1u;
             if (x.len > 0) {
                 ok = __all_sync(0xffffffffu, wait_or_abort(B_accfull(buf), (acc >> 1) & 1u, &s_abort));
                 if (!ok) break;
                 fence_after_sync();
                 ++acc;
             }
-            TO* out = static_cast<TO*>(a.out) + (MODE == EX_WEIGHT ? (size_t)x.e * a.N * a.K : 0) + (size_t)(x.i + w * 32) * (MODE == EX_WEIGHT ? (size_t)a.K : a.out_stride) + x.j;
-            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)(buf * pl.bn);
-            const int width = cols - x.j < pl.bn ? cols - x.j : pl.bn, height = x.i_end - x.i - w * 32;
             const size_t os = MODE == EX_WEIGHT ? (size_t)a.K : a.out_stride;
-            if (MODE == EX_WEIGHT && a.accumulate) store_tile<TO, float, true>(out, os, height, width, src, x.len > 0, s_out[w], lane);
-            else store_tile<TO, TO, false>(out, os, height, width, src, x.len > 0, s_out[w], lane);
+            TO* out = static_cast<TO*>(a.out) + (MODE == EX_WEIGHT ? (size_t)x.e * a.N * a.K : 0) + (size_t)(x.i + w * 32) * os + x.j;
+            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + buf * (uint32_t)pl.bn;
+            const int width = cols - x.j < pl.bn ? cols - x.j : pl.bn, height = x.i_end - x.i - w * 32;
+            if (height > 0) {
+                if (MODE == EX_WEIGHT && a.accumulate) store_tile<TO, float, true>(out, os, height, width, src, x.len > 0, s_out[w], lane);
+                else store_tile<TO, TO, false>(out, os, height, width, src, x.len > 0, s_out[w], lane);
+            }
             if (x.len > 0) {
                 fence_before_sync();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(B_accempty(buf));
+                if (lane == 0) {
+                    if (rank == 0) mbar_arrive(B_accempty(buf));
+                    else mbar_arrive_peer_relaxed(bar_first + 8u * (3 * MM_MAX_STAGES + 2 + buf));       // (what was read is in registers: nothing to order)
+                }
             }
         }
     }
     fence_before_sync();
     __syncthreads();
+    if (PAIR) cluster_sync();                                  // no block goes while the other's copies, products or arrivals may still reach it
     if (tid == 0 && s_abort != 0 && a.status != nullptr) *a.status = 2u;
     if (warp == 2) {
         fence_after_sync();
-        tmem_dealloc(tmem, pl.tmem_cols);
+        tmem_dealloc<PAIR>(tmem, pl.tmem_cols);
     }
 }
 
@@ -408,53 +460,65 @@ bool mma_shape(const ExpertArgs& a, ec_dtype_t dtype, ec_dtype_t out_dtype, int 
     return mma::encode_tiled() != nullptr;
 }
 
-MmaPlan mma_plan(const ExpertArgs& a, int mode) {
+template <class TO, int MODE, bool PAIR>
+int launch_mma(const ExpertArgs& a, int bm, int bn, int sms, cudaStream_t st) {
+    constexpr int BLOCKS = PAIR ? 2 : 1;
     MmaPlan p = {};
-    const int cols = mode == EX_FORWARD ? a.N : a.K;
-    p.bm = MM_ROWS;
-    p.bn = 256;
-    while (p.bn > 64 && p.bn / 2 >= cols) p.bn /= 2;
-    p.a_bytes = MM_ROWS * MM_STEP * 2;
-    p.b_bytes = (uint32_t)p.bn * MM_STEP * 2;
+    p.bm = bm;
+    p.bn = bn;
+    p.a_bytes = (uint32_t)bm * MM_STEP * 2;
+    p.b_bytes = (uint32_t)(bn / BLOCKS) * MM_STEP * 2;
     p.stage_bytes = p.a_bytes + p.b_bytes;
-    p.tx_bytes = p.stage_bytes;
-    p.stages = (int)((200u * 1024u - 1024u) / p.stage_bytes);
+    const uint32_t beyond = (uint32_t)(MM_ROWS - bm) * MM_STEP * 2;              // what the products read behind a short A tile (not used)
+    p.stages = (int)((MM_SMEM - 1024u - beyond) / p.stage_bytes);
     if (p.stages > MM_MAX_STAGES) p.stages = MM_MAX_STAGES;
-    p.tmem_cols = (uint32_t)p.bn * 2;
-    p.idesc = mma::instr_desc(MM_ROWS, p.bn, mode == EX_WEIGHT, mode != EX_FORWARD);
-    p.smem = (uint32_t)p.stages * p.stage_bytes + 1024u;
-    return p;
-}
-
-template <class TO, int MODE>
-int launch_mma(const ExpertArgs& a, cudaStream_t st) {
-    const MmaPlan p = mma_plan(a, MODE);
+    p.tmem_cols = (uint32_t)bn * 2;
+    p.idesc = mma::instr_desc(MM_ROWS * BLOCKS, bn, MODE == EX_WEIGHT, MODE != EX_FORWARD);
+    p.smem = (uint32_t)p.stages * p.stage_bytes + beyond + 1024u;
     CUtensorMap ma, mb;
     const size_t NK = (size_t)a.N * a.K;
     bool ok;
     if (MODE == EX_FORWARD)
-        ok = mma::make_map(&ma, a.x, 2, a.K, a.T, 1, a.x_stride, 0, MM_STEP, (unsigned)p.bm) &&
-             mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, MM_STEP, (unsigned)p.bn);
+        ok = mma::make_map(&ma, a.x, 2, a.K, a.T, 1, a.x_stride, 0, MM_STEP, (unsigned)bm) &&
+             mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, MM_STEP, (unsigned)(bn / BLOCKS));
     else if (MODE == EX_INPUT)
-        ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, MM_STEP, (unsigned)p.bm) &&
+        ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, MM_STEP, (unsigned)bm) &&
              mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, 64, MM_STEP);
     else
         ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, 64, MM_STEP) &&
              mma::make_map(&mb, a.x, 2, a.K, a.T, 1, a.x_stride, 0, 64, MM_STEP);
     if (!ok) return EC_ERR_CUDA;
+    int dev = 0;
+    EC_CUDA(cudaGetDevice(&dev));
+    static std::atomic<uint64_t> ready{0};                     // devices on which the shared-memory limit is raised
+    if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1u)) {
+        EC_CUDA(cudaFuncSetAttribute(expert_mma_kernel<TO, MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MM_SMEM));
+        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
+    }
+    const size_t jt = ((size_t)(MODE == EX_FORWARD ? a.N : a.K) + bn - 1) / bn, rows = (size_t)bm * BLOCKS;
+    const size_t most = MODE == EX_WEIGHT ? (size_t)a.E * ((a.N + MM_ROWS * BLOCKS - 1) / (MM_ROWS * BLOCKS)) * jt : (a.T / rows + a.E) * jt;
+    const size_t workers = most < (size_t)sms / BLOCKS ? most : (size_t)sms / BLOCKS;
+    cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = BLOCKS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = PAIR ? 1 : 0; cfg.stream = st;
+    cfg.gridDim = dim3((unsigned)(workers * BLOCKS)); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = p.smem;
+    EC_CUDA(cudaLaunchKernelEx(&cfg, expert_mma_kernel<TO, MODE, PAIR>, ma, mb, a, p));
+    return EC_OK;
+}
+
+template <class TO, int MODE>
+int launch_mma(const ExpertArgs& a, cudaStream_t st) {
     int dev = 0, sms = 0;
     EC_CUDA(cudaGetDevice(&dev));
     EC_CUDA(cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    static std::atomic<uint64_t> ready{0};                     // devices on which the shared-memory limit is raised
-    if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1u)) {
-        EC_CUDA(cudaFuncSetAttribute(expert_mma_kernel<TO, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024));
-        if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
-    }
-    const size_t jt = ((size_t)(MODE == EX_FORWARD ? a.N : a.K) + p.bn - 1) / p.bn;
-    const size_t most = MODE == EX_WEIGHT ? (size_t)a.E * ((a.N + MM_ROWS - 1) / MM_ROWS) * jt : (a.T / p.bm + a.E) * jt;
-    expert_mma_kernel<TO, MODE><<<(unsigned)(most < (size_t)sms ? most : sms), MM_THREADS, p.smem, st>>>(ma, mb, a, p);
-    EC_CUDA(cudaGetLastError());
-    return EC_OK;
+    const int cols = MODE == EX_FORWARD ? a.N : a.K;
+    const size_t mean = MODE == EX_WEIGHT ? (size_t)a.N : a.T / a.E;          // rows of the result an expert has (weight grad: exactly)
+    int bn = 256;
+    while (bn > 64 && bn / 2 >= cols) bn /= 2;
+    if (mean > 128 && bn >= 128) return launch_mma<TO, MODE, true>(a, MM_ROWS, bn, sms, st);
+    return launch_mma<TO, MODE, false>(a, MM_ROWS, bn, sms, st);
 }
 
 template <int MODE>
