@@ -29,11 +29,11 @@ struct ExpertArgs {
     int E, N, K, accumulate;
 };
 
-// The row ranges of the experts in shared memory, and the number of row tiles of `tile` rows before each expert (`plus` more
-// for every expert).  All threads of the block; returns false (and block 0 says so in *status) if displs does not ascend
+// The row ranges of the experts in shared memory, and the number of row tiles of `tile` rows (at least `least`) before each
+// expert.  All threads of the block; returns false (and block 0 says so in *status) if displs does not ascend
 // within [0, T].
 template <int THREADS>
-__device__ bool expert_ranges(const ExpertArgs& a, int tile, int plus, int* s_row, int* s_tile, int* s_warp) {
+__device__ bool expert_ranges(const ExpertArgs& a, int tile, int least, int* s_row, int* s_tile, int* s_warp) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     bool ok = true;
     int carry = 0;
@@ -47,7 +47,8 @@ __device__ bool expert_ranges(const ExpertArgs& a, int tile, int plus, int* s_ro
             } else {
                 s_row[e] = (int)b;
                 if (e == a.E - 1) s_row[a.E] = (int)d;
-                n = (int)((d - b + tile - 1) / tile) + plus;
+                n = (int)((d - b + tile - 1) / tile);
+                n = n > least ? n : least;
             }
         }
         int inc = n;
@@ -93,7 +94,7 @@ __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertA
     __shared__ float s_a[SC_STEP][SC_TILE + 4], s_b[SC_STEP][SC_TILE + 4];
     if (!expert_ranges<SC_THREADS>(a, SC_TILE, 0, s_row, s_tile, s_warp)) return;
     const int rows_out = MODE == EX_WEIGHT ? a.N : 0, cols_out = MODE == EX_FORWARD ? a.N : a.K;
-    const int jt = (cols_out + SC_TILE - 1) / SC_TILE, it = (rows_out + SC_TILE - 1) / SC_TILE;
+    const int jt = (cols_out + SC_TILE - 1) / SC_TILE, it = MODE == EX_WEIGHT ? (rows_out + SC_TILE - 1) / SC_TILE : 1;
     const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * it * jt : (long long)s_tile[a.E] * jt;
     const int tid = threadIdx.x, ti = tid / 16, tj = tid % 16;
     const TI* x = static_cast<const TI*>(a.x);
@@ -171,7 +172,7 @@ __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertA
 //                          where rows are the reduction (weight grad) the last step's foreign rows are overwritten with
 //                          zeros before the product, both operands, since they may hold infinities or NaN;
 //   issuer (one thread, of a pair's first block)  multiplies a landed stage, as it lies, into one of two accumulators in tensor memory;
-//   epilogue (four warps)  reads the finished accumulator while the next tile's products run, rounds once and writes it out
+//   epilogue (4, 8 or 16 warps)  reads the finished accumulator while the next products run, rounds once and writes it out
 //                          through a small transposing buffer, so that a warp's stores cover whole 128-byte lines.
 // A pair multiplies 256 x bn: each block brings its 128 rows of A and half of B's columns, and the tensor cores read the other
 // half of B from the other block.  A block alone needs 16 + 32 KB of operands, written and read, for the 512 cycles of a step at
@@ -182,13 +183,22 @@ __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertA
 // Every wait is bounded; a wait that gives up raises a flag that all roles poll, the block sets *status to 2, waits for its
 // copies in flight, frees its tensor memory and returns.
 
-constexpr int MM_THREADS = 256, MM_ROWS = 128, MM_STEP = 64, MM_MAX_STAGES = 12;
-constexpr int MM_PITCH = 144;                                  // bytes of a 128-byte row in the transposing buffer
-constexpr int MM_TILE_COST = 3;                                // writing a tile out, in reduction steps (for sharing out the weight grad)
-constexpr uint32_t MM_SMEM = 200 * 1024;                       // dynamic shared memory, beside 27 KB of static
+constexpr int MM_ROWS = 128, MM_STEP = 64, MM_MAX_STAGES = 12;
+// bf16 results: the accumulator is complete when it is read; four epilogue warps, eight in the weight grad, whose reductions are
+// as short as an expert's rows.  fp32 results: the tensor core's additions into an accumulator truncate - the error grows by about
+// 3.7e-8 of the sum with every 16 of the reduction (8192 rows: 2e-5) - so every MM_CHUNK steps the accumulator is
+// added, rounded to nearest, to sums in the registers of eight epilogue warps (512 rows: 1.2e-6 -> 2.2e-7; 32-bit
+// library product 2.6e-7), while the tensor core goes on in the other accumulator.
+constexpr int MM_CHUNK = 4;
+template <class TO> __host__ __device__ constexpr int mm_epilogue(int mode) { return sizeof(TO) == 4 || mode == EX_WEIGHT ? 8 : 4; }
+template <class TO> __host__ __device__ constexpr int mm_threads(int mode) { return 128 + 32 * mm_epilogue<TO>(mode); }
+constexpr uint32_t MM_SMEM = 217 * 1024;                       // dynamic shared memory at most, beside 9 KB of static
+constexpr int MM_PITCH = 144;                                  // bytes of a 128-byte row in the transposing buffer (bf16; fp32: 128, swizzled)
+template <class TO> __host__ __device__ constexpr uint32_t mm_out_bytes(int mode) { return mm_epilogue<TO>(mode) * 32u * (sizeof(TO) == 4 ? 128 : MM_PITCH); }
+constexpr int MM_MIN_STEPS = 6;                                // what writing a tile out costs, in steps: no tile of the weight grad costs less
 
 struct MmaPlan {
-    int bm, bn, stages;                                        // rows of A a block takes (<= 128), columns of the tile, ring stages
+    int bn, stages;                                            // columns of a tile, ring stages
     uint32_t a_bytes, b_bytes, stage_bytes, tmem_cols, idesc, smem;
 };
 
@@ -246,24 +256,45 @@ __device__ __forceinline__ void store_tile(TO* out, size_t stride, int height, i
     }
 }
 
+// 32 columns of a warp's 32 rows whose sums are in registers, into the transposing buffer: rows of 128 bytes, their 16-byte pieces
+// swizzled as a bulk tensor store expects them (and so that neither side meets a bank twice).
+__device__ __forceinline__ void stage_sums(const float (&a)[16], const float (&b)[16], unsigned char* buf, int lane) {
+    float4* row = reinterpret_cast<float4*>(buf + lane * 128);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        row[q ^ (lane & 7)] = make_float4(a[4 * q], a[4 * q + 1], a[4 * q + 2], a[4 * q + 3]);
+        row[(q + 4) ^ (lane & 7)] = make_float4(b[4 * q], b[4 * q + 1], b[4 * q + 2], b[4 * q + 3]);
+    }
+}
+__device__ __forceinline__ void store_staged(float* out, size_t stride, int height, int width, const unsigned char* buf, int lane) {
+    const int c = (lane & 7) * 4;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {                              // eight lanes a row, four rows a step
+        const int r = q * 4 + (lane >> 3);
+        if (r < height && c < width)
+            __stcs(reinterpret_cast<float4*>(out + (size_t)r * stride + c), *(reinterpret_cast<const float4*>(buf + r * 128) + ((lane & 7) ^ (r & 7))));
+    }
+}
+
 template <class TO, int MODE, bool PAIR>
-__global__ void __launch_bounds__(MM_THREADS, 1)
-expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const ExpertArgs a, const MmaPlan pl) {
+__global__ void __launch_bounds__(mm_threads<TO>(MODE), 1)
+expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_out,
+                  const ExpertArgs a, const MmaPlan pl) {
     using namespace mma;
+    constexpr int BLOCKS = PAIR ? 2 : 1, EPI = mm_epilogue<TO>(MODE);
     extern __shared__ unsigned char mm_raw[];
-    __shared__ int s_row[MAX_EXPERTS + 1], s_tile[MAX_EXPERTS + 1], s_warp[MM_THREADS / 32];
+    __shared__ int s_row[MAX_EXPERTS + 1], s_tile[MAX_EXPERTS + 1], s_warp[mm_threads<TO>(MODE) / 32];
     __shared__ __align__(8) uint64_t s_bar[3 * MM_MAX_STAGES + 4];
     __shared__ uint32_t s_tmem;
     __shared__ volatile int s_abort;
-    __shared__ __align__(16) unsigned char s_out[4][32 * MM_PITCH];
-    constexpr int BLOCKS = PAIR ? 2 : 1;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u;
     const uint32_t worker = blockIdx.x / BLOCKS, workers = gridDim.x / BLOCKS;
-    const int tile_rows = pl.bm * BLOCKS;                      // rows of a tile
-    if (!expert_ranges<MM_THREADS>(a, MODE == EX_WEIGHT ? MM_STEP : tile_rows, MODE == EX_WEIGHT ? MM_TILE_COST : 0, s_row, s_tile, s_warp)) return;
+    constexpr int tile_rows = MM_ROWS * BLOCKS;                // rows of a tile
+    if (!expert_ranges<mm_threads<TO>(MODE)>(a, MODE == EX_WEIGHT ? MM_STEP : tile_rows, MODE == EX_WEIGHT ? MM_MIN_STEPS : 0, s_row, s_tile, s_warp)) return;
 
     unsigned char* sm = mm_raw + ((1024u - (smem_u32(mm_raw) & 1023u)) & 1023u);
+    auto out_buffer = [&](int w) { return sm + (size_t)pl.stages * pl.stage_bytes + w * (mm_out_bytes<TO>(MODE) / EPI); };
     const uint32_t stage0 = smem_u32(sm), bar0 = smem_u32(s_bar), nst = (uint32_t)pl.stages;
     auto B_full = [&](uint32_t s) { return bar0 + 8u * s; };                               // used: the first block's
     auto B_empty = [&](uint32_t s) { return bar0 + 8u * (MM_MAX_STAGES + s); };
@@ -272,7 +303,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     auto B_accempty = [&](uint32_t b) { return bar0 + 8u * (3 * MM_MAX_STAGES + 2 + b); }; // used: the first block's
     if (tid == 0) {
         for (uint32_t s = 0; s < nst; ++s) { mbar_init(B_full(s), BLOCKS); mbar_init(B_empty(s), 1); mbar_init(B_tail(s), 1); }
-        for (uint32_t b = 0; b < 2; ++b) { mbar_init(B_accfull(b), 1); mbar_init(B_accempty(b), 4 * BLOCKS); }
+        for (uint32_t b = 0; b < 2; ++b) { mbar_init(B_accfull(b), 1); mbar_init(B_accempty(b), EPI * BLOCKS); }
         s_abort = 0;
         mbar_init_fence();
     }
@@ -319,14 +350,15 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         } else {
             x.e = expert_of(s_tile, a.E, (int)(t / jt));
             const int mt = s_tile[x.e + 1] - s_tile[x.e], q = (int)(t - (long long)s_tile[x.e] * jt);
-            x.i = s_row[x.e] + (q % mt) * tile_rows + (int)rank * pl.bm;
-            x.i_end = x.i + pl.bm < s_row[x.e + 1] ? x.i + pl.bm : s_row[x.e + 1];
+            x.i = s_row[x.e] + (q % mt) * tile_rows + (int)rank * MM_ROWS;
+            x.i_end = x.i + MM_ROWS < s_row[x.e + 1] ? x.i + MM_ROWS : s_row[x.e + 1];
             x.j = (q / mt) * pl.bn;
             x.len = MODE == EX_FORWARD ? a.K : a.N;
         }
         return x;
     };
 
+    constexpr int CHUNK = sizeof(TO) == 4 ? MM_CHUNK * MM_STEP : 0;           // (0: the whole reduction in one accumulator)
     bool ok = true;
     const uint32_t bar_first = PAIR ? peer_address(bar0, 0) : bar0;             // the barriers of the pair's first block
     if (warp == 0 && lane == 0) {
@@ -369,21 +401,43 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (long long t = t0; t < t1 && ok; t += dt) {
             const int len = tile_of(t).len;
             if (len == 0) continue;
-            const uint32_t buf = acc & 1u, d = tmem + buf * (uint32_t)pl.bn;
-            if (acc >= 2 && !wait_or_abort(B_accempty(buf), ((acc >> 1) - 1) & 1u, &s_abort)) break;
-            fence_after_sync();
-            for (int l = 0; l < len; l += MM_STEP) {
-                if (!wait_or_abort(B_full(s), phase, &s_abort)) { ok = false; break; }
-                fence_after_sync();
-                const uint32_t sa = stage0 + s * pl.stage_bytes;
-                const uint64_t da = base_a + (sa >> 4), db = base_b + ((sa + pl.a_bytes) >> 4);
+            int steps = len / MM_STEP;                         // whole steps left, then `rest` groups of 16
+            uint32_t rest = (uint32_t)(len % MM_STEP + 15) / 16u;
+            while (ok && (steps > 0 || rest > 0)) {            // an accumulator: the whole reduction, or CHUNK of it
+                if (acc >= 2 && !wait_or_abort(B_accempty(acc & 1u), ((acc >> 1) - 1) & 1u, &s_abort)) { ok = false; break; }
+                const uint32_t d = tmem + (acc & 1u) * (uint32_t)pl.bn;
+                uint32_t add = 0;
+                const int now = CHUNK > 0 && steps > MM_CHUNK ? MM_CHUNK : steps;
+                for (int i = 0; i < now; ++i) {
+                    if (!wait_or_abort(B_full(s), phase, &s_abort)) { ok = false; break; }
+                    fence_after_sync();
+                    const uint32_t sa = stage0 + s * pl.stage_bytes;
+                    const uint64_t da = base_a + (sa >> 4), db = base_b + ((sa + pl.a_bytes) >> 4);
 #pragma unroll
-                for (uint32_t k = 0; k < MM_STEP / 16; ++k) mma_bf16<PAIR>(d, da + k * STEP_A, db + k * STEP_B, pl.idesc, l > 0 || k > 0 ? 1u : 0u);
-                mma_commit<PAIR>(B_empty(s));
-                if (++s == nst) { s = 0; phase ^= 1u; }
+                    for (uint32_t k = 0; k < MM_STEP / 16; ++k) {
+                        mma_bf16<PAIR>(d, da + k * STEP_A, db + k * STEP_B, pl.idesc, add);
+                        add = 1;
+                    }
+                    mma_commit<PAIR>(B_empty(s));
+                    if (++s == nst) { s = 0; phase ^= 1u; }
+                }
+                steps -= now;
+                if (ok && steps == 0 && rest > 0 && (CHUNK == 0 || now < MM_CHUNK)) {
+                    if (!wait_or_abort(B_full(s), phase, &s_abort)) { ok = false; break; }
+                    fence_after_sync();
+                    const uint32_t sa = stage0 + s * pl.stage_bytes;
+                    const uint64_t da = base_a + (sa >> 4), db = base_b + ((sa + pl.a_bytes) >> 4);
+                    for (uint32_t k = 0; k < rest; ++k) {
+                        mma_bf16<PAIR>(d, da + k * STEP_A, db + k * STEP_B, pl.idesc, add);
+                        add = 1;
+                    }
+                    mma_commit<PAIR>(B_empty(s));
+                    if (++s == nst) { s = 0; phase ^= 1u; }
+                    rest = 0;
+                }
+                if (ok) mma_commit<PAIR>(B_accfull(acc & 1u));
+                ++acc;
             }
-            if (ok) mma_commit<PAIR>(B_accfull(buf));
-            ++acc;
         }
     } else if (MODE == EX_WEIGHT && warp == 3) {
         // the last step's rows of the next expert: zeros in both operands
@@ -395,11 +449,10 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             ok = __all_sync(0xffffffffu, wait_or_abort(B_tail(s), (tails >> s) & 1u, &s_abort));       // (the warp goes on, or leaves, together)
             if (!ok) break;
             tails ^= 1u << s;
-            const int boxes = (int)(pl.stage_bytes / 8192u), items = (MM_STEP - keep) * 8;
-            for (int q = lane; q < boxes * items; q += 32) {
-                const int box = q / items, p = q - box * items;
-                *reinterpret_cast<uint4*>(sm + (size_t)s * pl.stage_bytes + box * 8192 + keep * 128 + p * 16) = make_uint4(0, 0, 0, 0);
-            }
+            const int pieces = (((keep + 15) & ~15) - keep) * 8;                           // 16-byte pieces up to the end of the last 16 rows that are multiplied
+            unsigned char* from = sm + (size_t)s * pl.stage_bytes + keep * 128;
+            for (uint32_t box = 0; box < pl.stage_bytes; box += 8192u)
+                for (int q = lane; q < pieces; q += 32) *reinterpret_cast<uint4*>(from + box + q * 16) = make_uint4(0, 0, 0, 0);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) {
@@ -409,35 +462,80 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             if (++s == nst) s = 0;
         }
     } else if (warp >= 4) {
-        const int w = warp - 4;
+        const int w = warp & 3, half = (warp - 4) >> 2;         // the warp's 32 rows; its part of the columns
         uint32_t acc = 0;
         for (long long t = t0; t < t1 && ok; t += dt) {
             const Tile x = tile_of(t);
             if (MODE == EX_WEIGHT && x.len == 0 && a.accumulate) continue;
-            const uint32_t buf = acc & 1u;
-            if (x.len > 0) {
-                ok = __all_sync(0xffffffffu, wait_or_abort(B_accfull(buf), (acc >> 1) & 1u, &s_abort));
-                if (!ok) break;
-                fence_after_sync();
-                ++acc;
-            }
+            const int part = pl.bn / (EPI / 4), first = half * part;
             const size_t os = MODE == EX_WEIGHT ? (size_t)a.K : a.out_stride;
-            TO* out = static_cast<TO*>(a.out) + (MODE == EX_WEIGHT ? (size_t)x.e * a.N * a.K : 0) + (size_t)(x.i + w * 32) * os + x.j;
-            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + buf * (uint32_t)pl.bn;
-            const int width = cols - x.j < pl.bn ? cols - x.j : pl.bn, height = x.i_end - x.i - w * 32;
-            if (height > 0) {
-                if (MODE == EX_WEIGHT && a.accumulate) store_tile<TO, float, true>(out, os, height, width, src, x.len > 0, s_out[w], lane);
-                else store_tile<TO, TO, false>(out, os, height, width, src, x.len > 0, s_out[w], lane);
-            }
-            if (x.len > 0) {
+            TO* out = static_cast<TO*>(a.out) + (MODE == EX_WEIGHT ? (size_t)x.e * a.N * a.K : 0) + (size_t)(x.i + w * 32) * os + x.j + first;
+            const uint32_t src = tmem + ((uint32_t)(w * 32) << 16) + (uint32_t)first;
+            const int left = cols - x.j - first, width = left < part ? left : part, height = x.i_end - x.i - w * 32;
+            auto filled = [&] {                                // the next accumulator
+                ok = __all_sync(0xffffffffu, wait_or_abort(B_accfull(acc & 1u), (acc >> 1) & 1u, &s_abort));
+                fence_after_sync();
+                return ok;
+            };
+            auto taken = [&] {
                 fence_before_sync();
                 __syncwarp();
                 if (lane == 0) {
-                    if (rank == 0) mbar_arrive(B_accempty(buf));
-                    else mbar_arrive_peer_relaxed(bar_first + 8u * (3 * MM_MAX_STAGES + 2 + buf));       // (what was read is in registers: nothing to order)
+                    const uint32_t bar = 3 * MM_MAX_STAGES + 2 + (acc & 1u);
+                    if (rank == 0) mbar_arrive(bar0 + 8u * bar);
+                    else mbar_arrive_peer_relaxed(bar_first + 8u * bar);                   // (what was read is in registers: nothing to order)
                 }
+                ++acc;
+            };
+            if constexpr (sizeof(TO) == 4) {
+                float sum[8][16] = {};
+                for (int l = 0; l < x.len; l += CHUNK) {
+                    if (!filled()) break;
+#pragma unroll
+                    for (int p = 0; p < 8; ++p) {
+                        if (p * 16 < part) {
+                            uint32_t v[16];
+                            tmem_ld16(src + (acc & 1u) * (uint32_t)pl.bn + p * 16, v);
+                            tmem_ld_wait();
+#pragma unroll
+                            for (int q = 0; q < 16; ++q) sum[p][q] += __uint_as_float(v[q]);
+                        }
+                    }
+                    taken();
+                }
+                if (!ok) break;
+                unsigned char* buf = out_buffer(warp - 4);
+#pragma unroll
+                for (int p = 0; p < 4; ++p) {
+                    if (p * 32 < width && height > 0) {
+                        if (MODE == EX_WEIGHT && lane == 0) tma_store_source_free();       // (the buffer's last store has read it)
+                        __syncwarp();
+                        stage_sums(sum[2 * p], sum[2 * p + 1], buf, lane);
+                        if (MODE == EX_WEIGHT) {
+                            fence_async_smem();
+                            __syncwarp();
+                            if (lane == 0) {
+                                const int jx = x.j + first + p * 32, iy = x.i + w * 32;
+                                if (a.accumulate) tma_store_3d<true>(&map_out, smem_u32(buf), jx, iy, x.e);
+                                else tma_store_3d<false>(&map_out, smem_u32(buf), jx, iy, x.e);
+                            }
+                        } else {
+                            __syncwarp();
+                            store_staged(out + p * 32, os, height, width - p * 32, buf, lane);
+                        }
+                    }
+                }
+            } else {
+                if (x.len > 0 && !filled()) break;
+                const uint32_t from = src + (acc & 1u) * (uint32_t)pl.bn;
+                if (height > 0 && width > 0) {
+                    if (MODE == EX_WEIGHT && a.accumulate) store_tile<TO, float, true>(out, os, height, width, from, x.len > 0, out_buffer(warp - 4), lane);
+                    else store_tile<TO, TO, false>(out, os, height, width, from, x.len > 0, out_buffer(warp - 4), lane);
+                }
+                if (x.len > 0) taken();
             }
         }
+        if (sizeof(TO) == 4 && MODE == EX_WEIGHT && lane == 0) tma_store_done();
     }
     fence_before_sync();
     __syncthreads();
@@ -461,32 +559,33 @@ bool mma_shape(const ExpertArgs& a, ec_dtype_t dtype, ec_dtype_t out_dtype, int 
 }
 
 template <class TO, int MODE, bool PAIR>
-int launch_mma(const ExpertArgs& a, int bm, int bn, int sms, cudaStream_t st) {
+int launch_mma(const ExpertArgs& a, int bn, int sms, cudaStream_t st) {
     constexpr int BLOCKS = PAIR ? 2 : 1;
     MmaPlan p = {};
-    p.bm = bm;
     p.bn = bn;
-    p.a_bytes = (uint32_t)bm * MM_STEP * 2;
+    p.a_bytes = MM_ROWS * MM_STEP * 2;
     p.b_bytes = (uint32_t)(bn / BLOCKS) * MM_STEP * 2;
     p.stage_bytes = p.a_bytes + p.b_bytes;
-    const uint32_t beyond = (uint32_t)(MM_ROWS - bm) * MM_STEP * 2;              // what the products read behind a short A tile (not used)
-    p.stages = (int)((MM_SMEM - 1024u - beyond) / p.stage_bytes);
+    p.stages = (int)((MM_SMEM - 1024u - mm_out_bytes<TO>(MODE)) / p.stage_bytes);
     if (p.stages > MM_MAX_STAGES) p.stages = MM_MAX_STAGES;
     p.tmem_cols = (uint32_t)bn * 2;
     p.idesc = mma::instr_desc(MM_ROWS * BLOCKS, bn, MODE == EX_WEIGHT, MODE != EX_FORWARD);
-    p.smem = (uint32_t)p.stages * p.stage_bytes + beyond + 1024u;
+    p.smem = (uint32_t)p.stages * p.stage_bytes + mm_out_bytes<TO>(MODE) + 1024u;
     CUtensorMap ma, mb;
     const size_t NK = (size_t)a.N * a.K;
     bool ok;
     if (MODE == EX_FORWARD)
-        ok = mma::make_map(&ma, a.x, 2, a.K, a.T, 1, a.x_stride, 0, MM_STEP, (unsigned)bm) &&
+        ok = mma::make_map(&ma, a.x, 2, a.K, a.T, 1, a.x_stride, 0, MM_STEP, MM_ROWS) &&
              mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, MM_STEP, (unsigned)(bn / BLOCKS));
     else if (MODE == EX_INPUT)
-        ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, MM_STEP, (unsigned)bm) &&
+        ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, MM_STEP, MM_ROWS) &&
              mma::make_map(&mb, a.w, 3, a.K, a.N, a.E, a.K, NK, 64, MM_STEP);
     else
         ok = mma::make_map(&ma, a.dy, 2, a.N, a.T, 1, a.dy_stride, 0, 64, MM_STEP) &&
              mma::make_map(&mb, a.x, 2, a.K, a.T, 1, a.x_stride, 0, 64, MM_STEP);
+    CUtensorMap mo = ma;                                       // (used by the fp32 weight grad alone)
+    if (ok && MODE == EX_WEIGHT && sizeof(TO) == 4)
+        ok = mma::make_map(&mo, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, a.out, 3, a.K, a.N, a.E, a.K, NK, 32, 32);
     if (!ok) return EC_ERR_CUDA;
     int dev = 0;
     EC_CUDA(cudaGetDevice(&dev));
@@ -495,7 +594,7 @@ int launch_mma(const ExpertArgs& a, int bm, int bn, int sms, cudaStream_t st) {
         EC_CUDA(cudaFuncSetAttribute(expert_mma_kernel<TO, MODE, PAIR>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MM_SMEM));
         if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
     }
-    const size_t jt = ((size_t)(MODE == EX_FORWARD ? a.N : a.K) + bn - 1) / bn, rows = (size_t)bm * BLOCKS;
+    const size_t jt = ((size_t)(MODE == EX_FORWARD ? a.N : a.K) + bn - 1) / bn, rows = (size_t)MM_ROWS * BLOCKS;
     const size_t most = MODE == EX_WEIGHT ? (size_t)a.E * ((a.N + MM_ROWS * BLOCKS - 1) / (MM_ROWS * BLOCKS)) * jt : (a.T / rows + a.E) * jt;
     const size_t workers = most < (size_t)sms / BLOCKS ? most : (size_t)sms / BLOCKS;
     cudaLaunchConfig_t cfg = {};
@@ -503,8 +602,8 @@ int launch_mma(const ExpertArgs& a, int bm, int bn, int sms, cudaStream_t st) {
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = BLOCKS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = PAIR ? 1 : 0; cfg.stream = st;
-    cfg.gridDim = dim3((unsigned)(workers * BLOCKS)); cfg.blockDim = dim3(MM_THREADS); cfg.dynamicSmemBytes = p.smem;
-    EC_CUDA(cudaLaunchKernelEx(&cfg, expert_mma_kernel<TO, MODE, PAIR>, ma, mb, a, p));
+    cfg.gridDim = dim3((unsigned)(workers * BLOCKS)); cfg.blockDim = dim3(mm_threads<TO>(MODE)); cfg.dynamicSmemBytes = p.smem;
+    EC_CUDA(cudaLaunchKernelEx(&cfg, expert_mma_kernel<TO, MODE, PAIR>, ma, mb, mo, a, p));
     return EC_OK;
 }
 
@@ -517,8 +616,14 @@ int launch_mma(const ExpertArgs& a, cudaStream_t st) {
     const size_t mean = MODE == EX_WEIGHT ? (size_t)a.N : a.T / a.E;          // rows of the result an expert has (weight grad: exactly)
     int bn = 256;
     while (bn > 64 && bn / 2 >= cols) bn /= 2;
-    if (mean > 128 && bn >= 128) return launch_mma<TO, MODE, true>(a, MM_ROWS, bn, sms, st);
-    return launch_mma<TO, MODE, false>(a, MM_ROWS, bn, sms, st);
+    if (mean > 128 && bn >= 128) return launch_mma<TO, MODE, true>(a, bn, sms, st);
+    // Few rows an expert: the weights are what is read, so the tiles are narrow enough to put every SM to work on them, in one round
+    // (64 rows, 32 experts of 512 x 1024, us with 256 / 128 / 64 columns: 12.4 / 10.4 / 14.5).
+    if (MODE != EX_WEIGHT) {
+        const size_t busy = a.T < (size_t)a.E ? a.T : (size_t)a.E;
+        while (bn > 64 && busy * ((cols + bn / 2 - 1) / (bn / 2)) <= (size_t)sms) bn /= 2;
+    }
+    return launch_mma<TO, MODE, false>(a, bn, sms, st);
 }
 
 template <int MODE>

@@ -99,6 +99,21 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map
             ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
+// A box of shared memory to global memory (ADD: added to what is there, fp32, rounded to nearest), one thread.  What the map
+// leaves outside is not written.
+template <bool ADD>
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+    if constexpr (ADD)
+        asm volatile("cp.reduce.async.bulk.tensor.3d.global.shared::cta.add.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                     ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    else
+        asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%2, %3, %4}], [%1];"
+                     ::"l"(map), "r"(src), "r"(x), "r"(y), "r"(z) : "memory");
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void tma_store_source_free() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+__device__ __forceinline__ void tma_store_done() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
 // PAIR: the same columns in both blocks of a pair; one warp of each calls it.
 template <bool PAIR>
 __device__ __forceinline__ void tmem_alloc(uint32_t dst_smem, uint32_t ncols) {
@@ -177,10 +192,19 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32]) {
         : "r"(taddr)
         : "memory");
 }
+// 16 of them.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr)
+        : "memory");
+}
 __device__ __forceinline__ void tmem_ld_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
-// Tensor map of a bf16 array of 2 or 3 dimensions (innermost first; strides in elements), copied in swizzled boxes of
-// box0 x box1 values.  The driver's encoder is looked up through the runtime: the library links no libcuda.
+// Tensor map of an array (without a type: bf16) of 2 or 3 dimensions, innermost first, strides in elements, copied in swizzled
+// boxes of box0 x box1 values.  The driver's encoder is looked up through the runtime: the library links no libcuda.
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
                                   const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
                                   CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -196,16 +220,19 @@ inline EncodeTiledFn encode_tiled() {
     }();
     return fn;
 }
-inline bool make_map(CUtensorMap* map, const void* base, int dims, size_t n0, size_t n1, size_t n2, size_t stride1, size_t stride2,
-                     unsigned box0, unsigned box1) {
+inline bool make_map(CUtensorMap* map, CUtensorMapDataType type, size_t size_of, const void* base, int dims, size_t n0, size_t n1, size_t n2,
+                     size_t stride1, size_t stride2, unsigned box0, unsigned box1) {
     const EncodeTiledFn fn = encode_tiled();
     if (fn == nullptr) return false;
     const cuuint64_t size[3] = {n0, n1, n2};
-    const cuuint64_t stride[2] = {stride1 * 2, stride2 * 2};
+    const cuuint64_t stride[2] = {stride1 * size_of, stride2 * size_of};
     const cuuint32_t box[3] = {box0, box1, 1}, step[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)dims, const_cast<void*>(base), size, stride, box, step,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+    return fn(map, type, (cuuint32_t)dims, const_cast<void*>(base), size, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+inline bool make_map(CUtensorMap* map, const void* base, int dims, size_t n0, size_t n1, size_t n2, size_t stride1, size_t stride2,
+                     unsigned box0, unsigned box1) {
+    return make_map(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, n0, n1, n2, stride1, stride2, box0, box1);
 }
 
 }  // namespace mma
