@@ -29,11 +29,10 @@ struct ExpertArgs {
     int E, N, K, accumulate;
 };
 
-// The row ranges of the experts in shared memory, and the number of row tiles of `tile` rows (at least `least`) before each
-// expert.  All threads of the block; returns false (and block 0 says so in *status) if displs does not ascend
+// The row ranges of the experts in shared memory, and the number of row tiles of `tile` rows before each expert.  All threads of the block; returns false (and block 0 says so in *status) if displs does not ascend
 // within [0, T].
 template <int THREADS>
-__device__ bool expert_ranges(const ExpertArgs& a, int tile, int least, int* s_row, int* s_tile, int* s_warp) {
+__device__ bool expert_ranges(const ExpertArgs& a, int tile, int* s_row, int* s_tile, int* s_warp) {
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     bool ok = true;
     int carry = 0;
@@ -48,7 +47,6 @@ __device__ bool expert_ranges(const ExpertArgs& a, int tile, int least, int* s_r
                 s_row[e] = (int)b;
                 if (e == a.E - 1) s_row[a.E] = (int)d;
                 n = (int)((d - b + tile - 1) / tile);
-                n = n > least ? n : least;
             }
         }
         int inc = n;
@@ -92,7 +90,7 @@ template <class TI, class TO, int MODE>
 __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertArgs a) {
     __shared__ int s_row[MAX_EXPERTS + 1], s_tile[MAX_EXPERTS + 1], s_warp[SC_THREADS / 32];
     __shared__ float s_a[SC_STEP][SC_TILE + 4], s_b[SC_STEP][SC_TILE + 4];
-    if (!expert_ranges<SC_THREADS>(a, SC_TILE, 0, s_row, s_tile, s_warp)) return;
+    if (!expert_ranges<SC_THREADS>(a, SC_TILE, s_row, s_tile, s_warp)) return;
     const int rows_out = MODE == EX_WEIGHT ? a.N : 0, cols_out = MODE == EX_FORWARD ? a.N : a.K;
     const int jt = (cols_out + SC_TILE - 1) / SC_TILE, it = MODE == EX_WEIGHT ? (rows_out + SC_TILE - 1) / SC_TILE : 1;
     const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * it * jt : (long long)s_tile[a.E] * jt;
@@ -186,16 +184,19 @@ __global__ void __launch_bounds__(SC_THREADS) expert_scalar_kernel(const ExpertA
 constexpr int MM_ROWS = 128, MM_STEP = 64, MM_MAX_STAGES = 12;
 // bf16 results: the accumulator is complete when it is read; four epilogue warps, eight in the weight grad, whose reductions are
 // as short as an expert's rows.  fp32 results: the tensor core's additions into an accumulator truncate - the error grows by about
-// 3.7e-8 of the sum with every 16 of the reduction (8192 rows: 2e-5) - so every MM_CHUNK steps the accumulator is
-// added, rounded to nearest, to sums in the registers of eight epilogue warps (512 rows: 1.2e-6 -> 2.2e-7; 32-bit
+// 3.7e-8 of the sum with every 16 of the reduction (8192 rows: 2e-5) - so every MM_CHUNK steps of 64 the accumulator is
+// added, rounded to nearest, to sums in the registers of eight epilogue warps (512 rows: 1.2e-6 -> 4.1e-7, every 4 steps: 2.2e-7; 32-bit
 // library product 2.6e-7), while the tensor core goes on in the other accumulator.
-constexpr int MM_CHUNK = 4;
+constexpr int MM_CHUNK = 8;
 template <class TO> __host__ __device__ constexpr int mm_epilogue(int mode) { return sizeof(TO) == 4 || mode == EX_WEIGHT ? 8 : 4; }
 template <class TO> __host__ __device__ constexpr int mm_threads(int mode) { return 128 + 32 * mm_epilogue<TO>(mode); }
 constexpr uint32_t MM_SMEM = 217 * 1024;                       // dynamic shared memory at most, beside 9 KB of static
 constexpr int MM_PITCH = 144;                                  // bytes of a 128-byte row in the transposing buffer (bf16; fp32: 128, swizzled)
 template <class TO> __host__ __device__ constexpr uint32_t mm_out_bytes(int mode) { return mm_epilogue<TO>(mode) * 32u * (sizeof(TO) == 4 ? 128 : MM_PITCH); }
-constexpr int MM_MIN_STEPS = 6;                                // what writing a tile out costs, in steps: no tile of the weight grad costs less
+// The weight grad takes the experts by falling number of rows, up to this many experts: tiles that run side by side then cost
+// about the same and read the same rows, which stay in L2 (16 experts of 2048 rows, 1024 x 2048, fp32: 117 us; with a run of tiles a
+// worker, all experts at once, 179).
+constexpr int MM_SORT = 256;
 
 struct MmaPlan {
     int bn, stages;                                            // columns of a tile, ring stages
@@ -291,7 +292,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u;
     const uint32_t worker = blockIdx.x / BLOCKS, workers = gridDim.x / BLOCKS;
     constexpr int tile_rows = MM_ROWS * BLOCKS;                // rows of a tile
-    if (!expert_ranges<mm_threads<TO>(MODE)>(a, MODE == EX_WEIGHT ? MM_STEP : tile_rows, MODE == EX_WEIGHT ? MM_MIN_STEPS : 0, s_row, s_tile, s_warp)) return;
+    if (!expert_ranges<mm_threads<TO>(MODE)>(a, tile_rows, s_row, s_tile, s_warp)) return;
 
     unsigned char* sm = mm_raw + ((1024u - (smem_u32(mm_raw) & 1023u)) & 1023u);
     auto out_buffer = [&](int w) { return sm + (size_t)pl.stages * pl.stage_bytes + w * (mm_out_bytes<TO>(MODE) / EPI); };
@@ -317,32 +318,30 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     // the tiles: for each expert, down the rows first
     const int cols = MODE == EX_FORWARD ? a.N : a.K, jt = (cols + pl.bn - 1) / pl.bn;
     const int wt = (a.N + MM_ROWS * BLOCKS - 1) / (MM_ROWS * BLOCKS);
-    long long t0 = worker, t1, dt = workers;
+    const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * wt * jt : (long long)s_tile[a.E] * jt;
     if (MODE == EX_WEIGHT) {
-        // Tiles of one expert cost the same, those of another expert more or less: every worker takes a run of tiles of about
-        // the same cost.  s_tile[e] = cost of one tile of each expert before e.
-        const long long per = (long long)wt * jt, all = per * s_tile[a.E];
-        auto first_from = [&](long long cost) {                // first tile that begins at `cost` or later
-            int lo = 0, hi = a.E - 1;
-            while (lo < hi) {
-                const int m = (lo + hi + 1) / 2;
-                if (per * s_tile[m] <= cost) lo = m; else hi = m - 1;
+        for (int e = tid; e < a.E; e += mm_threads<TO>(MODE)) {
+            int at = e;
+            if (a.E <= MM_SORT) {
+                const int n = s_row[e + 1] - s_row[e];
+                at = 0;
+                for (int f = 0; f < a.E; ++f) {
+                    const int m = s_row[f + 1] - s_row[f];
+                    at += m > n || (m == n && f < e) ? 1 : 0;
+                }
             }
-            const long long c = s_tile[lo + 1] - s_tile[lo], q = (cost - per * s_tile[lo] + c - 1) / c;
-            return lo * per + (q < per ? q : per);
-        };
-        t0 = first_from(all * worker / workers);
-        t1 = first_from(all * (worker + 1) / workers);
-        dt = 1;
-    } else {
-        t1 = (long long)s_tile[a.E] * jt;
+            s_tile[at] = e;                                    // (the weight grad has no row tiles)
+        }
+        __syncthreads();
     }
+    // The worker's i-th tile; every second round of the weight grad goes backwards, so that who had the larger tile gets the smaller.
+    auto nth = [&](long long i) { return i * workers + (MODE == EX_WEIGHT && (i & 1) ? workers - 1 - worker : worker); };
     struct Tile { int e, i, i_end, j, len; };                  // expert, the block's first result row, end of its rows, first column, reduction length
     auto tile_of = [&](long long t) {
         Tile x;
         if (MODE == EX_WEIGHT) {
-            x.e = (int)(t / ((long long)wt * jt));
-            const int q = (int)(t - (long long)x.e * wt * jt);
+            const int k = (int)(t / ((long long)wt * jt)), q = (int)(t - (long long)k * wt * jt);
+            x.e = s_tile[k];
             x.i = (q % wt) * (MM_ROWS * BLOCKS) + (int)rank * MM_ROWS;
             x.i_end = x.i + MM_ROWS < a.N ? x.i + MM_ROWS : a.N;
             x.j = (q / wt) * pl.bn;
@@ -364,7 +363,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (warp == 0 && lane == 0) {
         const int bh = pl.bn / BLOCKS;                         // columns of B the block brings
         uint32_t s = 0, use = 0;                               // the next stage, times the ring has been filled
-        for (long long t = t0; t < t1 && ok; t += dt) {
+        for (long long i = 0, t; (t = nth(i)) < tiles && ok; ++i) {
             const Tile x = tile_of(t);
             const int jb = x.j + (int)rank * bh;
             for (int l = 0; l < x.len; l += MM_STEP) {
@@ -398,7 +397,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         const uint64_t base_a = operand_desc(0, MODE == EX_WEIGHT ? 8192u : 16u), base_b = operand_desc(0, MODE == EX_FORWARD ? 16u : 8192u);
         constexpr uint32_t STEP_A = (MODE == EX_WEIGHT ? 2048u : 32u) >> 4, STEP_B = (MODE == EX_FORWARD ? 32u : 2048u) >> 4;
         uint32_t s = 0, phase = 0, acc = 0;                    // the next stage and its parity, accumulators filled
-        for (long long t = t0; t < t1 && ok; t += dt) {
+        for (long long i = 0, t; (t = nth(i)) < tiles && ok; ++i) {
             const int len = tile_of(t).len;
             if (len == 0) continue;
             int steps = len / MM_STEP;                         // whole steps left, then `rest` groups of 16
@@ -442,7 +441,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     } else if (MODE == EX_WEIGHT && warp == 3) {
         // the last step's rows of the next expert: zeros in both operands
         uint32_t s = 0, tails = 0;                             // the next stage, parity of each stage's tail barrier
-        for (long long t = t0; t < t1 && ok; t += dt) {
+        for (long long i = 0, t; (t = nth(i)) < tiles && ok; ++i) {
             const int len = tile_of(t).len, keep = len % MM_STEP;
             s = (s + (uint32_t)(len / MM_STEP)) % nst;
             if (keep == 0) continue;
@@ -464,7 +463,7 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     } else if (warp >= 4) {
         const int w = warp & 3, half = (warp - 4) >> 2;         // the warp's 32 rows; its part of the columns
         uint32_t acc = 0;
-        for (long long t = t0; t < t1 && ok; t += dt) {
+        for (long long i = 0, t; (t = nth(i)) < tiles && ok; ++i) {
             const Tile x = tile_of(t);
             if (MODE == EX_WEIGHT && x.len == 0 && a.accumulate) continue;
             const int part = pl.bn / (EPI / 4), first = half * part;
@@ -616,7 +615,14 @@ int launch_mma(const ExpertArgs& a, cudaStream_t st) {
     const size_t mean = MODE == EX_WEIGHT ? (size_t)a.N : a.T / a.E;          // rows of the result an expert has (weight grad: exactly)
     int bn = 256;
     while (bn > 64 && bn / 2 >= cols) bn /= 2;
-    if (mean > 128 && bn >= 128) return launch_mma<TO, MODE, true>(a, bn, sms, st);
+    if (mean > 128 && bn >= 128) {
+        // A step of a pair takes 640 cycles at 256 columns and, bound by shared memory, 400 at 128: narrower tiles pay where they
+        // fill a round better (weight grad, 8192 rows of one expert, 1024 x 2048: 61 -> 55 us).
+        const size_t rows = MODE == EX_WEIGHT ? (size_t)a.E * ((a.N + 255) / 256) : a.T / 256 + ((size_t)a.E + 1) / 2, workers = (size_t)sms / 2;
+        auto cost = [&](int n) { return (rows * ((cols + n - 1) / n) + workers - 1) / workers * (n == 256 ? 640 : 400); };
+        if (bn == 256 && cost(128) < cost(256)) bn = 128;
+        return launch_mma<TO, MODE, true>(a, bn, sms, st);
+    }
     // Few rows an expert: the weights are what is read, so the tiles are narrow enough to put every SM to work on them, in one round
     // (64 rows, 32 experts of 512 x 1024, us with 256 / 128 / 64 columns: 12.4 / 10.4 / 14.5).
     if (MODE != EX_WEIGHT) {

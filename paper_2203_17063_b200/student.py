@@ -1,0 +1,141 @@
+"""A language-model student distilled from a teacher's top logits, data-parallel over P simulated ranks.
+
+The model: token embedding, one layer of experts (each row goes to one of E experts) with a residual connection, output
+head.  Every rank has its own tokens; its gradients - of the embedding, the experts and the head - lie one behind the
+other in one fp32 vector, the rank's buffer of a stale-synchronous allreduce: a rank that is not fresh in a step leaves the
+buffer it delivered before, as long as that is not older than the slack allows (Algorithm 1 of the paper).
+
+Every step of a rank:
+    x      = scale * table[token]                     embed_lookup
+    y      = W_e x   for the rows of expert e         expert_forward        (rows sorted by expert)
+    logits = H (x + y)                                expert_forward, one expert
+    loss, dlogits                                     distill_step
+    dH, dh, dW_e, dx, dtable                          expert_weight_grad, expert_input_grad, embed_grad
+and then one ssp_apply over the P buffers and a gradient step on the fp32 parameters.
+
+``python -m paper_2203_17063_b200.student`` trains a small one on synthetic data and prints the loss.
+"""
+from __future__ import annotations
+
+import argparse
+import math
+
+import torch
+
+from . import binding as ec
+
+
+class Student:
+    """Parameters in fp32 (one vector, as the rank buffers) with bf16 copies that the operators read."""
+
+    def __init__(self, P: int, V: int, D: int, E: int, rows: int, lr: float, temperature: float = 1.0, segment: int = 4096,
+                 seed: int = 0, device: str = "cuda"):
+        self.P, self.V, self.D, self.E, self.rows, self.lr, self.temperature = P, V, D, E, rows, lr, temperature
+        self.scale = math.sqrt(D)
+        g = torch.Generator().manual_seed(seed)
+        shapes = [(V, D), (E, D, D), (1, V, D)]
+        std = [1.0 / D, 0.5 / math.sqrt(D), 1.0 / math.sqrt(D)]
+        self.sizes = [math.prod(s) for s in shapes]
+        self.n = sum(self.sizes)
+        self.master = torch.cat([torch.randn(n, generator=g) * s for n, s in zip(self.sizes, std)]).to(device)
+        self.router = torch.randn(E, D, generator=g).to(device, torch.bfloat16)
+        self._copy = torch.empty(self.n, dtype=torch.bfloat16, device=device)
+        self.table, self.experts, self.head = self._views(self._copy)
+        self._copy.copy_(self.master)
+        self.buffers = [torch.zeros(self.n, device=device) for _ in range(P)]        # what each rank has delivered
+        self.allreduce = ec.Allreduce(P, self.n, ec.F32, ec.SUM, segment, device=device)
+        S = self.allreduce.S
+        self.clock = 0
+        self.age = [0] * P                                                            # clock of each rank's last contribution
+        self.clocks = torch.zeros(S, P, dtype=torch.int32, device=device)           # clock of each contribution
+        self.sum = torch.zeros(self.n, device=device)
+        self.wait = torch.zeros(S, dtype=torch.int32, device=device)
+        # work arrays of one rank's step
+        bf = dict(dtype=torch.bfloat16, device=device)
+        self.x, self.y, self.h, self.dh, self.dx = (torch.empty(rows, D, **bf) for _ in range(5))
+        self.logits = torch.empty(rows, V, **bf)                                      # the gradient takes their place
+        self.loss, self.lse = torch.empty(rows, device=device), torch.empty(rows, device=device)
+        self.weight = torch.full((rows,), 1.0 / (P * rows), device=device)
+        self.one = torch.tensor([0, rows], device=device)
+        self.workspace = torch.empty(ec.embed_grad_workspace_bytes(rows, V, D), dtype=torch.uint8, device=device)
+
+    def _views(self, flat: torch.Tensor):
+        a, b, c = torch.split(flat, self.sizes)
+        return a.view(self.V, self.D), b.view(self.E, self.D, self.D), c.view(1, self.V, self.D)
+
+    def rank_gradient(self, r: int, tokens, top_index, top_logit) -> torch.Tensor:
+        """Gradient of rank r's share of the loss into its buffer; returns the rows' losses.  Tokens below 0 are padding."""
+        ec.embed_lookup(self.table, tokens, self.x, self.scale)
+        expert = (self.x @ self.router.T).argmax(1)                                   # routing is not trained here
+        order = torch.sort(expert, stable=True).indices
+        displs = torch.zeros(self.E + 1, dtype=torch.int64, device=tokens.device)
+        displs[1:] = torch.cumsum(torch.bincount(expert, minlength=self.E), 0)
+        tokens, top_index, top_logit = tokens[order], top_index[order], top_logit[order]
+        ec.embed_lookup(self.table, tokens, self.x, self.scale)                       # the rows again, sorted by expert
+        ec.expert_forward(self.x, displs, self.experts, self.y)
+        torch.add(self.x, self.y, out=self.h)
+        ec.expert_forward(self.h, self.one, self.head, self.logits)
+        ec.distill_step(self.logits, top_index, top_logit, self.loss, self.lse, self.logits, self.temperature, self.weight)
+        d_table, d_experts, d_head = self._views(self.buffers[r])
+        ec.expert_weight_grad(self.logits, self.h, self.one, d_head)
+        ec.expert_input_grad(self.logits, self.one, self.head, self.dh)
+        ec.expert_weight_grad(self.dh, self.x, displs, d_experts)
+        ec.expert_input_grad(self.dh, displs, self.experts, self.dx)
+        self.dx += self.dh
+        ec.embed_grad(self.dx, tokens, d_table, self.workspace, self.scale)
+        return self.loss
+
+    def step(self, batches, fresh=None, slack: int = 0) -> torch.Tensor:
+        """One iteration.  batches[r] = (tokens, top_index, top_logit) of rank r; fresh[r] tells whether rank r delivers now
+        (None: all do).  A rank whose last contribution would be older than `slack` is waited for, i.e. computed in any case.
+        Returns the loss of the ranks that were computed, as a device scalar."""
+        self.clock += 1
+        total = torch.zeros((), device=self.master.device)
+        for r in range(self.P):
+            if fresh is None or fresh[r] or self.age[r] < max(1, self.clock - slack):
+                total += self.rank_gradient(r, *batches[r]).sum()
+                self.clocks[:, r] = self.clock
+                self.age[r] = self.clock
+        self.allreduce.ssp_apply(self.buffers, self.clocks, self.clock, slack, self.sum, wait_count=self.wait)
+        self.master.add_(self.sum, alpha=-self.lr)
+        self._copy.copy_(self.master)
+        return total
+
+
+def synthetic_batch(V: int, K: int, rows: int, seed: int, device: str = "cuda"):
+    """Tokens by a Zipf law, one in twenty padding, and the teacher's list of every token: a fixed function of its id."""
+    g = torch.Generator().manual_seed(seed)
+    u = torch.rand(rows, generator=g, dtype=torch.float64)
+    tokens = (torch.exp(u * math.log(V + 1.0)) - 1).long().clamp(0, V - 1)
+    pad = torch.rand(rows, generator=g) < 0.05
+    k = torch.arange(K)
+    index = (tokens[:, None] * 7919 + k * (V // K)) % V
+    logit = (4.0 - 0.25 * k).expand(rows, K).contiguous()
+    tokens[pad] = -1
+    index[pad] = -1
+    return tokens.to(device), index.to(torch.int32).to(device), logit.to(device)
+
+
+def main() -> None:
+    ap = argparse.ArgumentParser(description=__doc__.splitlines()[0])
+    ap.add_argument("--steps", type=int, default=20)
+    ap.add_argument("--ranks", type=int, default=4)
+    ap.add_argument("--rows", type=int, default=1024, help="tokens of a rank and step")
+    ap.add_argument("--vocabulary", type=int, default=8192)
+    ap.add_argument("--width", type=int, default=256)
+    ap.add_argument("--experts", type=int, default=8)
+    ap.add_argument("--top", type=int, default=16)
+    ap.add_argument("--slack", type=int, default=2)
+    a = ap.parse_args()
+    s = Student(a.ranks, a.vocabulary, a.width, a.experts, a.rows, lr=0.5)
+    g = torch.Generator().manual_seed(1)
+    for t in range(a.steps):
+        batches = [synthetic_batch(a.vocabulary, a.top, a.rows, 1000 * t + r) for r in range(a.ranks)]
+        fresh = (torch.rand(a.ranks, generator=g) < 0.75).tolist()
+        loss = s.step(batches, fresh, a.slack)
+        share = sum(age == s.clock for age in s.age) / a.ranks
+        print(f"step {t + 1}: loss {loss.item() / max(share, 1e-9):.4f}, {share:.0%} of the ranks fresh")
+
+
+if __name__ == "__main__":
+    main()

@@ -1,0 +1,77 @@
+"""The operators together: one training step of the student against automatic differentiation in 64 bits, and training."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from paper_2203_17063_b200 import student as st
+
+
+def loss64(s, params, tokens, index, logit, weight):
+    """The student's loss by its definition in 64 bits; params: the three parameter arrays, requiring gradients."""
+    table, experts, head = params
+    there = tokens >= 0
+    x = table[tokens.clamp_min(0)] * s.scale * there[:, None]
+    expert = (x.detach().bfloat16() @ s.router.T).argmax(1)
+    h = x + torch.einsum("ndk,nk->nd", experts[expert], x)
+    logp = torch.log_softmax(h @ head[0].T / s.temperature, 1)
+    a = torch.where(index >= 0, logit.double() / s.temperature, torch.tensor(-1e30, dtype=torch.float64, device="cuda"))
+    p = torch.softmax(a, 1) * (index >= 0)
+    logq = logp.gather(1, index.clamp_min(0).long())
+    keep = (index >= 0).any(1)
+    terms = torch.where(p > 0, p * (torch.log(p.clamp_min(1e-300)) - logq), torch.zeros_like(p)).sum(1)
+    return (weight.double() * terms * keep).sum()
+
+
+def test_gradient_of_a_step(cuda_device):
+    """Eight roundings to bf16 (x, y, h, logits, their gradient, dh, dx twice), each at most 2^-8 of a value, lie between the
+    parameters and a gradient: 8 * 2^-8 of its norm."""
+    V, D, E, rows, K = 512, 64, 4, 300, 8
+    s = st.Student(1, V, D, E, rows, lr=0.1, seed=3)
+    tokens, index, logit = st.synthetic_batch(V, K, rows, 5)
+    loss = s.rank_gradient(0, tokens, index, logit).sum().item()
+    params = [v.detach().double().requires_grad_() for v in s._views(s._copy)]
+    want = loss64(s, params, tokens, index, logit, s.weight)
+    want.backward()
+    torch.cuda.synchronize()
+    assert abs(loss - want.item()) <= 8 * 2.0 ** -8 * abs(want.item())
+    for got, p in zip(s._views(s.buffers[0]), params):
+        assert (got.double() - p.grad).norm() <= 8 * 2.0 ** -8 * p.grad.norm()
+    assert not s._views(s.buffers[0])[0][torch.bincount(tokens[tokens >= 0], minlength=V) == 0].any()
+
+
+def test_training_lowers_the_loss_and_repeats(cuda_device):
+    def run():
+        s = st.Student(3, 1024, 64, 4, 256, lr=0.5, seed=1)
+        losses, computed = [], []
+        for t in range(12):
+            batches = [st.synthetic_batch(1024, 8, 256, 10 * t + r) for r in range(3)]
+            losses.append(s.step(batches, fresh=[True, t % 2 == 0, t % 3 == 0], slack=1))
+            computed.append(sum(age == s.clock for age in s.age))
+        torch.cuda.synchronize()
+        assert not s.wait.any()
+        return torch.stack(losses), s.master.clone(), s.clocks.clone(), computed
+
+    a, b = run(), run()
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])                  # bit for bit
+    per_rank = [x / n for x, n in zip(a[0].tolist(), a[3])]                     # loss of a rank that was computed
+    assert math.isfinite(per_rank[-1]) and sum(per_rank[-3:]) < sum(per_rank[:3])
+    assert int(a[2].min()) >= 11                                                # slack 1: no contribution older than one step
+
+
+def test_ranks_sum_up_to_one(cuda_device):
+    """Two ranks with half of the rows each take the step that one rank takes with all of them (another order of summation:
+    the gradients agree to the roundings of test_gradient_of_a_step, most of which are the same in both)."""
+    V, D, E, K = 512, 64, 4, 8
+    whole = st.Student(1, V, D, E, 400, lr=1.0, seed=2)
+    split = st.Student(2, V, D, E, 200, lr=1.0, seed=2)
+    tokens, index, logit = st.synthetic_batch(V, K, 400, 9)
+    start = whole.master.clone()
+    l1 = whole.step([(tokens, index, logit)])
+    l2 = split.step([(tokens[:200], index[:200], logit[:200]), (tokens[200:], index[200:], logit[200:])])
+    torch.cuda.synchronize()
+    assert abs(l1.item() - l2.item()) <= 8 * 2.0 ** -8 * abs(l1.item())
+    d1, d2 = whole.master - start, split.master - start
+    assert (d1 - d2).norm() <= 8 * 2.0 ** -8 * d1.norm()
