@@ -245,7 +245,7 @@ __device__ __forceinline__ uint32_t peer_address(const void* p, uint32_t rank) {
 }
 __device__ __forceinline__ uint32_t peer_load(uint32_t address) {
     uint32_t x;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(address) : "memory");
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(x) : "r"(address));
     return x;
 }
 __device__ __forceinline__ void peer_store(uint32_t address, uint32_t x, uint32_t y) {
@@ -273,39 +273,50 @@ __global__ void __launch_bounds__(CS_THREADS) sort_cluster_kernel(const ClusterS
     for (int pass = 0; pass < a.passes; ++pass) {
         const int shift = pass * a.bits;
         const uint32_t bins = 1u << a.bits;
-        for (int d = tid; d < CS_WARPS * SORT_BINS; d += CS_THREADS) (&s_n[0][0])[d] = 0;
-        __syncthreads();
+        for (uint32_t d = lane; d < bins; d += 32) s_n[w][d] = 0;  // (a warp counts in its own row)
+        __syncwarp();
+        uint32_t same[ITEMS];
+#pragma unroll
+        for (int q = 0; q < ITEMS; ++q)                            // items past the end: a digit of their own
+            same[q] = __match_any_sync(0xffffffffu, base + q * 32 < a.T ? (key[q] >> shift) & (bins - 1) : bins);
 #pragma unroll
         for (int q = 0; q < ITEMS; ++q) {
             const bool in = base + q * 32 < a.T;
-            const uint32_t d = in ? (key[q] >> shift) & (bins - 1) : bins;      // items past the end: a digit of their own
-            const uint32_t same = __match_any_sync(0xffffffffu, d);
-            const uint32_t below = __popc(same & ((1u << lane) - 1u));
+            const uint32_t d = (key[q] >> shift) & (bins - 1), below = __popc(same[q] & ((1u << lane) - 1u));
             const uint32_t old = in ? s_n[w][d] : 0u;
             __syncwarp();
-            if (in && below == 0) s_n[w][d] = old + __popc(same);
+            if (in && below == 0) s_n[w][d] = old + __popc(same[q]);
             __syncwarp();
             at[q] = old + below;
         }
         __syncthreads();
         if (tid < (int)bins) {                                     // a thread per digit: the warps' counts become their offsets
-            uint32_t sum = 0;
+            uint32_t n[CS_WARPS], sum = 0;
+#pragma unroll
+            for (int q = 0; q < CS_WARPS; ++q) n[q] = s_n[q][tid];
 #pragma unroll
             for (int q = 0; q < CS_WARPS; ++q) {
-                const uint32_t n = s_n[q][tid];
                 s_n[q][tid] = sum;
-                sum += n;
+                sum += n[q];
             }
             s_total[tid] = sum;
         }
-        sort_cluster_sync();
         uint32_t before = 0, all = 0;
-        if (tid < (int)bins)
-            for (uint32_t r = 0; r < blocks; ++r) {
-                const uint32_t n = peer_load(peer_address(&s_total[tid], r));
-                before += r < rank ? n : 0u;
-                all += n;
+        if (blocks == 1) {
+            if (tid < (int)bins) all = s_total[tid];
+        } else {
+            sort_cluster_sync();
+            if (tid < (int)bins) {
+                uint32_t n[8];
+#pragma unroll
+                for (uint32_t r = 0; r < 8; ++r) n[r] = r < blocks ? peer_load(peer_address(&s_total[tid], r)) : 0u;
+#pragma unroll
+                for (uint32_t r = 0; r < 8; ++r) {
+                    before += r < rank ? n[r] : 0u;
+                    all += n[r];
+                }
             }
+        }
         const uint32_t inc = warp_inclusive(all, lane);
         if (lane == 31) s_warp[w] = inc;
         __syncthreads();
@@ -324,7 +335,8 @@ __global__ void __launch_bounds__(CS_THREADS) sort_cluster_kernel(const ClusterS
                 peer_store(peer_address(&s_items[p % HOLD], p / HOLD), key[q], pos[q]);
             }
         }
-        sort_cluster_sync();                                       // (the last one: no block goes while another may read its counts)
+        if (blocks > 1) sort_cluster_sync();                       // (the last one: no block goes while another may read its counts)
+        else __syncthreads();
         if (!last) {
 #pragma unroll
             for (int q = 0; q < ITEMS; ++q) {
