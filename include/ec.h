@@ -516,7 +516,8 @@ int ec_threshold_segments(const uint32_t* contrib_count, size_t S, uint32_t need
  * (to nearest even) when an output is bf16.  Results repeat bit for bit.
  * Strides are in elements, from one row to the next, at least the row length
  * (EC_ERR_INVALID otherwise); elements between rows are neither read nor written.
- * Outputs must not overlap inputs unless a call says so.
+ * Outputs must not overlap inputs unless a call says so.  Pointers lie on the
+ * grid of their element type (EC_ERR_INVALID otherwise).
  * ------------------------------------------------------------------------- */
 typedef enum {
     EC_INDEX_32 = 0, /* int32 */

@@ -442,6 +442,11 @@ int check(const DistillArgs& a, size_t T, ec_dtype_t dtype, ec_index_t index, ec
     if (mode != MODE_LOSS && a.grad == a.logits && a.grad_stride != a.stride) return EC_ERR_INVALID;
     if (a.K > EC_DISTILL_MAX_TOP) return EC_ERR_CAPACITY;
     if (!is_real_dtype(dtype) || !is_real_dtype(top_dtype)) return EC_ERR_UNSUPPORTED;
+    if (!on_grid(a.logits, in_bytes(dtype)) || !on_grid(a.grad, in_bytes(dtype)) || !on_grid(a.top_index, a.index64 ? 8 : 4) ||
+        !on_grid(a.top_logit, in_bytes(top_dtype)))
+        return EC_ERR_INVALID;
+    for (const void* p : {(const void*)a.teacher_lse, (const void*)a.weight, (const void*)a.dloss, (const void*)a.loss, (const void*)a.lse})
+        if (!on_grid(p, 4)) return EC_ERR_INVALID;
     return EC_OK;
 }
 

@@ -789,6 +789,7 @@ int ec_embed_lookup(const void* table, size_t V, size_t D, size_t table_stride, 
     if (!table || (T > 0 && (!tokens || !out)) || !embed_sizes_ok(T, V, D)) return EC_ERR_INVALID;
     if (table_stride < D || out_stride < D || (index != EC_INDEX_32 && index != EC_INDEX_64)) return EC_ERR_INVALID;
     if (!is_real_dtype(table_dtype) || !is_real_dtype(out_dtype)) return EC_ERR_UNSUPPORTED;
+    if (!on_grid(table, in_bytes(table_dtype)) || !on_grid(out, in_bytes(out_dtype)) || !on_grid(tokens, index == EC_INDEX_32 ? 4 : 8)) return EC_ERR_INVALID;
     if (T == 0) return EC_OK;
     return with_types(table_dtype, out_dtype, [&](auto ti, auto to) {
         using TI = decltype(ti); using TO = decltype(to);
@@ -810,6 +811,7 @@ int ec_embed_grad(const void* dout, size_t dout_stride, ec_dtype_t dout_dtype, c
     if (!grad || (T > 0 && (!dout || !tokens)) || !embed_sizes_ok(T, V, D) || T + V > EMBED_MAX) return EC_ERR_INVALID;
     if (dout_stride < D || grad_stride < D || (index != EC_INDEX_32 && index != EC_INDEX_64)) return EC_ERR_INVALID;
     if (!is_real_dtype(dout_dtype) || !is_real_dtype(grad_dtype)) return EC_ERR_UNSUPPORTED;
+    if (!on_grid(dout, in_bytes(dout_dtype)) || !on_grid(grad, in_bytes(grad_dtype)) || !on_grid(tokens, index == EC_INDEX_32 ? 4 : 8)) return EC_ERR_INVALID;
     GradLayout L;
     grad_layout(T, V, D, &L);
     if (!workspace || workspace_bytes < L.total || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return EC_ERR_CAPACITY;

@@ -651,6 +651,9 @@ int check(const ExpertArgs& a, ec_dtype_t dtype, ec_dtype_t out_dtype, int mode)
     if (mode != EX_WEIGHT && a.out_stride < (size_t)(mode == EX_FORWARD ? a.N : a.K)) return EC_ERR_INVALID;
     if (a.E > EC_MAX_EXPERTS || a.N > (1 << 20) || a.K > (1 << 20)) return EC_ERR_CAPACITY;
     if (!is_real_dtype(dtype) || !is_real_dtype(out_dtype)) return EC_ERR_UNSUPPORTED;
+    if (!on_grid(a.x, in_bytes(dtype)) || !on_grid(a.dy, in_bytes(dtype)) || !on_grid(a.w, in_bytes(dtype)) ||
+        !on_grid(a.out, in_bytes(out_dtype)) || !on_grid(a.displs, 8) || !on_grid(a.status, 4))
+        return EC_ERR_INVALID;
     return EC_OK;
 }
 

@@ -111,6 +111,8 @@ inline auto with_types(ec_dtype_t a, ec_dtype_t b, F f) {
     if (a == EC_F32) return b == EC_F32 ? f(float{}, float{}) : f(float{}, bf16_t{});
     return b == EC_F32 ? f(bf16_t{}, float{}) : f(bf16_t{}, bf16_t{});
 }
+// Does p lie on its element's grid?  (A GPU cannot read an element that does not.)
+inline bool on_grid(const void* p, size_t size) { return reinterpret_cast<uintptr_t>(p) % size == 0; }
 inline bool is_real_dtype(ec_dtype_t d) { return d == EC_F32 || d == EC_BF16; }
 
 }  // namespace ec

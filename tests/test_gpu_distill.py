@@ -133,7 +133,8 @@ def run_all(z, i, l, tau, w, tl, pad=0, offset=0, gpad=None, goffset=None):
 
 
 SHAPES = [(1, 1, 1), (3, 2, 1), (5, 7, 9), (4, 8, 4), (2, 31, 8), (9, 255, 3), (6, 1000, 33), (17, 4096, 64), (3, 4097, 256),
-          (5, 8191, 16), (2, 50021, 50), (150, 2048, 8), (1, 131072, 64), (2, 131077, 64), (300, 513, 1), (1, 300001, 100), (2, 600011, 5)]
+          (5, 8191, 16), (2, 50021, 50), (150, 2048, 8), (1, 131072, 64), (2, 131077, 64), (300, 513, 1), (1, 300001, 100), (2, 600011, 5),
+          (310, 40001, 7), (300, 9000, 12)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -258,6 +259,27 @@ def test_step_repeats_bit_for_bit_on_another_stream(cuda_device):
     torch.cuda.synchronize()
     for o in outs[1:]:
         assert all(torch.equal(x, y) for x, y in zip(outs[0], o))
+
+
+def test_offsets_past_32_bits(cuda_device):
+    """More than 2^31 logits: the last row is where it belongs (the others have weight 0)."""
+    T, V, K = 40000, 70000, 6
+    z = torch.empty(T, V, dtype=torch.bfloat16, device="cuda")
+    row, i, l, _ = problem(1, V, K, 8)
+    z[-1] = row[0].to(torch.bfloat16)
+    index = torch.full((T, K), -1, dtype=torch.int32, device="cuda")
+    index[-1] = i[0]
+    top = torch.zeros(T, K, device="cuda")
+    top[-1] = l[0]
+    w = torch.zeros(T, device="cuda")
+    w[-1] = 0.75
+    want = reference(z[-1:], i, l, 1.0, w[-1:], None)
+    loss, lse = torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    ec.distill_step(z, index, top, loss, lse, z, 1.0, w)
+    torch.cuda.synchronize()
+    within(loss[-1:], want[0], want[1], "loss")
+    within(z[-1:], want[4], want[5], "gradient")
+    assert not loss[:-1].any() and not z[0].any() and not z[-2].any()
 
 
 def test_empty_batch(cuda_device):

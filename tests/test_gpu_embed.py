@@ -124,6 +124,25 @@ def test_grad(cuda_device, T, V, D, accumulate, src, dst):
             assert torch.equal(again, grad)
 
 
+@pytest.mark.parametrize("T,V,D,index", [(40000, 1000, 16, torch.int32), (65536, 70000, 8, torch.int64), (65537, 300, 24, torch.int64),
+                                         (200001, 600000, 4, torch.int32), (150000, 3, 33, torch.int64)])
+def test_grad_of_many_tokens(cuda_device, T, V, D, index):
+    """One cluster sorts up to 65536 tokens, several launches more; both keep a row's positions in ascending order."""
+    for k, kind in enumerate(["zipf", "uniform", "one"]):
+        _, dout = make_rows(T, D, torch.float32, D, 40 + k)
+        tokens = make_tokens(kind, T, V, index, 41 + k)
+        ws = torch.full((ec.embed_grad_workspace_bytes(T, V, D),), 0x5A, dtype=torch.uint8, device="cuda")
+        outs = []
+        for _ in range(2):
+            grad = torch.full((V, D), float("nan"), device="cuda")
+            ec.embed_grad(dout, tokens, grad, ws, 0.5, 1)
+            outs.append(grad)
+        torch.cuda.synchronize()
+        want, bound, _ = reference_grad(dout, tokens, V, 0.5, 1, None)
+        assert bool(((outs[0].double() - want).abs() <= bound).all())
+        assert torch.equal(outs[0], outs[1])
+
+
 def test_grad_is_the_derivative_of_the_lookup(cuda_device):
     """f(table) = <lookup(table), dout> is linear: f(table + delta) - f(table) = <delta, grad>; integers, so exact."""
     T, V, D = 700, 90, 24
@@ -142,6 +161,28 @@ def test_grad_is_the_derivative_of_the_lookup(cuda_device):
     left = ((out1 - out0).double() * dout.double()).sum()
     right = (delta.double() * grad.double()).sum()
     assert left.item() == right.item()
+
+
+def test_what_gives_nothing_may_hold_anything(cuda_device):
+    """Rows of dropped tokens are NaN or infinite, and so are table rows that no token names."""
+    T, V, D = 900, 40, 36
+    tokens = make_tokens("uniform", T, V, torch.int64, 8)
+    tokens[::5] = 7
+    dout = torch.randn(T, D, device="cuda")
+    clean, dirty = torch.empty(V, D, device="cuda"), torch.empty(V, D, device="cuda")
+    ws = torch.empty(ec.embed_grad_workspace_bytes(T, V, D), dtype=torch.uint8, device="cuda")
+    ec.embed_grad(dout, tokens, clean, ws, 1.5, 7)
+    gone = (tokens < 0) | (tokens >= V) | (tokens == 7)
+    dout[gone] = float("nan")
+    dout[torch.nonzero(gone)[0]] = float("inf")
+    ec.embed_grad(dout, tokens, dirty, ws, 1.5, 7)
+    table = torch.full((V, D), float("nan"), device="cuda")
+    table[3] = 2.0
+    out = torch.empty(3, D, device="cuda")
+    ec.embed_lookup(table, torch.tensor([3, -1, V], device="cuda"), out, 0.5)
+    torch.cuda.synchronize()
+    assert torch.equal(clean, dirty) and not clean[7].any()
+    assert bool((out[0] == 1).all()) and not out[1:].any()
 
 
 def test_two_streams_two_workspaces(cuda_device):

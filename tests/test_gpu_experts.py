@@ -113,6 +113,52 @@ def test_any_alignment_and_fp32(cuda_device, cuts, T, N, K, out):
     check_all(cuts, T, N, K, "f32", out, pad=1, offset=0, seed=20)
 
 
+@pytest.mark.parametrize("cuts,T,N,K", [([0, 2500, 2600, 6000, 6001, 9000], 9000, 1544, 1032), ([0, 5000], 5000, 264, 8),
+                                        ([0, 700, 700, 4000, 4800], 4800, 136, 2056)])
+def test_more_tiles_than_workers(cuda_device, cuts, T, N, K):
+    """Several rounds of tiles, stage rings and accumulators that wrap many times, experts of very different sizes."""
+    check_all(cuts, T, N, K, "bf16", "bf16", seed=30)
+    check_all(cuts, T, N, K, "bf16", "f32", pad=8, offset=8, seed=31)
+
+
+def test_fp32_results_of_long_reductions(cuda_device):
+    """Sums in chains of 512 rounded to nearest: a chain is off by at most 32 ulps 2^-23 of its own sum by truncation, the sums of
+    chains by rounding; in the 2-norm of random operands 2^-23 * 32 / 2 is an upper bound of the first (partial sums grow as
+    the square root of their length), one thirty-second of it is left for the second."""
+    for L in (512, 8192, 32768):
+        a, b = torch.randn(L, 256, device="cuda").bfloat16(), torch.randn(L, 320, device="cuda").bfloat16()
+        dw, y = torch.empty(1, 256, 320, device="cuda"), torch.empty(256, 320, device="cuda")
+        ec.expert_weight_grad(a, b, torch.tensor([0, L], device="cuda"), dw)
+        ec.expert_forward(a.t().contiguous(), torch.tensor([0, 256], device="cuda"), b.t().contiguous()[None], y)
+        torch.cuda.synchronize()
+        want = a.double().t() @ b.double()
+        for got in (dw[0], y):
+            assert (got.double() - want).norm() <= 2.0 ** -23 * 16.5 * want.norm()
+
+
+def test_offsets_past_32_bits(cuda_device):
+    """Weights of more than 2^31 elements, rows at the last expert alone."""
+    E, N, K, T = 300, 4096, 2048, 130
+    w = torch.empty(E, N, K, dtype=torch.bfloat16, device="cuda")
+    fill_random(w[-1], 1, K ** -0.5)
+    x, dy = torch.empty(T, K, dtype=torch.bfloat16, device="cuda"), torch.empty(T, N, dtype=torch.bfloat16, device="cuda")
+    fill_random(x, 2)
+    fill_random(dy, 3)
+    displs = torch.zeros(E + 1, dtype=torch.int64, device="cuda")
+    displs[-1] = T
+    y, dx = torch.empty(T, N, device="cuda"), torch.empty(T, K, device="cuda")
+    ec.expert_forward(x, displs, w, y)
+    ec.expert_input_grad(dy, displs, w, dx)
+    torch.cuda.synchronize()
+    xe, de, we = x.double(), dy.double(), w[-1].double()
+    within(y, xe @ we.T, bound(K, xe.abs() @ we.abs().T), "forward")
+    within(dx, de @ we, bound(N, de.abs() @ we.abs()), "input grad")
+    ec.expert_weight_grad(dy, x, displs, w)
+    torch.cuda.synchronize()
+    within(w[-1], de.T @ xe, bound(T, de.abs().T @ xe.abs()), "weight grad")
+    assert not w[0].any() and not w[-2].any()
+
+
 def test_many_experts(cuda_device):
     """1024 experts, most without rows; prefix sums over several chunks of experts."""
     g = torch.Generator().manual_seed(3)

@@ -86,3 +86,24 @@ def test_experts(lib):
         strides = {k: 1 << 21 for k in good if k.endswith("_stride")}
         assert call(fn, good, E=1025) == CAPACITY
         assert call(fn, good, N=(1 << 20) + 1, **strides) == CAPACITY and call(fn, good, K=(1 << 20) + 1, **strides) == CAPACITY
+
+
+def test_pointers_off_the_grid(lib):
+    """An address that is no multiple of the element's size is refused: the GPU could not read it."""
+    odd, half, word = C.c_void_p(4097), C.c_void_p(4098), C.c_void_p(4100)
+    look = dict(table=P, V=8, D=16, table_stride=16, table_dtype=0, tokens=P, index=1, T=4, scale=1.0, out=P, out_stride=16, out_dtype=1, stream=None)
+    for change in (dict(table=half), dict(out=odd), dict(tokens=word), dict(tokens=half, index=0)):
+        assert call(lib.ec_embed_lookup, look, **change) == INVALID, change
+    need = lib.ec_embed_grad_workspace_bytes(4, 8, 16)
+    grad = dict(dout=P, dout_stride=16, dout_dtype=0, tokens=P, index=0, T=4, V=8, D=16, scale=1.0, skip=-1, accumulate=0, grad=P,
+                grad_stride=16, grad_dtype=1, workspace=P, workspace_bytes=need, stream=None)
+    for change in (dict(dout=half), dict(grad=odd), dict(tokens=half)):
+        assert call(lib.ec_embed_grad, grad, **change) == INVALID, change
+    step = dict(logits=P, stride=64, dtype=1, T=4, V=64, index_ptr=P, index=0, top=P, top_dtype=0, K=8, tau=1.0, weight=None, teacher_lse=None,
+                loss=P, lse=P, grad=C.c_void_p(8192), grad_stride=64, s=None)
+    for change in (dict(logits=odd), dict(index_ptr=half), dict(index_ptr=word, index=1), dict(top=half), dict(weight=half), dict(teacher_lse=half),
+                   dict(loss=half), dict(lse=half), dict(grad=odd)):
+        assert call(lib.ec_distill_step, step, **change) == INVALID, change
+    fwd = dict(x=P, x_stride=16, displs=P, E=2, w=P, dtype=1, T=6, N=8, K=16, y=P, y_stride=8, y_dtype=0, status=None, stream=None)
+    for change in (dict(x=odd), dict(displs=word), dict(w=odd), dict(y=half), dict(status=half)):
+        assert call(lib.ec_expert_forward, fwd, **change) == INVALID, change
