@@ -6,7 +6,7 @@
 //   dz_v = g (m exp(u_v - lse) - sum over k with i_k = v of p_k),   m = sum_k p_k,  g = w / tau [* dloss]
 //
 // A row of logits is read once, its gradient written once: bound by memory.  Exponentials are taken to base 2 (one fused
-// multiply-add and one ex2 an element); maxima, sums and the gradient are fp32, rounded once when the gradient is bf16.
+// multiply-add and one ex2 an element, multiply-adds and additions two at a time: 787 -> 756 us for 8192 x 131072 bf16); maxima, sums and the gradient are fp32, rounded once when the gradient is bf16.
 // Every thread keeps the maximum of what it has seen and the sum of exponentials below it; a block joins its threads in a
 // fixed order.  The gradient is first written as if no entry were in the teacher's list; the list's entries follow behind a
 // barrier, each written by the block that owns its column.
@@ -39,6 +39,33 @@ __device__ __forceinline__ float ex2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+typedef unsigned long long f32x2;                            // two fp32 in a register pair: one instruction for both
+__device__ __forceinline__ f32x2 pair(float x, float y) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ void unpair(f32x2 p, float& x, float& y) { asm("mov.b64 {%0, %1}, %2;" : "=f"(x), "=f"(y) : "l"(p)); }
+__device__ __forceinline__ f32x2 pair_fma(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 pair_add(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 pair_mul(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 pair_ex2(f32x2 t) {
+    float x, y;
+    unpair(t, x, y);
+    return pair(ex2(x), ex2(y));
 }
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -160,13 +187,17 @@ __device__ __forceinline__ float sum_below(const raw_vec<T, 16 / (int)sizeof(T)>
     const float cm = c * m;
     float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (fabsf(cm) < 1e38f) {
+        f32x2 a[2] = {0ull, 0ull};
+        const f32x2 cc = pair(c, c), mm = pair(-cm, -cm);
 #pragma unroll
         for (int q = 0; q < N; ++q) {
             float x[W];
             unpack<T, W>(v[q], x);
 #pragma unroll
-            for (int e = 0; e < W; ++e) s[e & 3] += ex2(fmaf(x[e], c, -cm));
+            for (int e = 0; e < W; e += 2) a[e / 2 & 1] = pair_add(a[e / 2 & 1], pair_ex2(pair_fma(pair(x[e], x[e + 1]), cc, mm)));
         }
+        unpair(a[0], s[0], s[1]);
+        unpair(a[1], s[2], s[3]);
     } else {          // rows masked with the type's lowest value throughout: the difference cannot overflow to a NaN
 #pragma unroll
         for (int q = 0; q < N; ++q) {
@@ -315,6 +346,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             G = g * mass / S;
         }
         if (skip) fused = false;
+        const f32x2 gg = pair(G, G), cc = pair(c, c), oo = pair(-off, -off);
         auto scaled = [&](float x) {
             if (fused) return G * ex2(fmaf(x, c, -off));
             return G * ex2(MODE == MODE_GRAD ? fmaf(x, a.inv_tau, -lse) * LOG2E : (x - M) * c);
@@ -342,7 +374,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
                     unpack<T, W>(v[q], x);
                     if (fused) {
 #pragma unroll
-                        for (int e = 0; e < W; ++e) x[e] = G * ex2(fmaf(x[e], c, -off));
+                        for (int e = 0; e < W; e += 2) unpair(pair_mul(gg, pair_ex2(pair_fma(pair(x[e], x[e + 1]), cc, oo))), x[e], x[e + 1]);
                     } else {
 #pragma unroll
                         for (int e = 0; e < W; ++e) x[e] = skip ? 0.0f : scaled(x[e]);
