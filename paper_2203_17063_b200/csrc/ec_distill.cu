@@ -5,9 +5,9 @@
 //   loss = w sum_k p_k (log p_k - u_{i_k} + lse)
 //   dz_v = g (m exp(u_v - lse) - sum over k with i_k = v of p_k),   m = sum_k p_k,  g = w / tau [* dloss]
 //
-// A row of logits is read once, its gradient written once: bound by memory.  Exponentials are taken to base 2 (one fused
-// multiply-add and one ex2 an element, multiply-adds and additions two at a time: 787 -> 756 us for 8192 x 131072 bf16); maxima, sums and the gradient are fp32, rounded once when the gradient is bf16.
-// Every thread keeps the maximum of what it has seen and the sum of exponentials below it; a block joins its threads in a
+// A row of logits is read once, its gradient written once: bound by memory.  Exponentials are taken to base 2: one fused
+// multiply-add and one ex2 an element, multiply-adds and additions two at a time (787 -> 756 us for 8192 x 131072 bf16).
+// Maxima, sums and the gradient are fp32, rounded once when the gradient is bf16.  Every thread keeps the maximum of what it has seen and the sum of exponentials below it; a block joins its threads in a
 // fixed order.  The gradient is first written as if no entry were in the teacher's list; the list's entries follow behind a
 // barrier, each written by the block that owns its column.
 
@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             }
         }
     };
-    load(0, MODE == MODE_STEP);
+    load(0, false);                                                // (only what lies between the first and the last batch is read again)
     const float edge = mine.edge >= 0 ? unpack_one<T>(z[mine.edge]) : -INFINITY;
     float weight = a.weight != nullptr ? a.weight[t] : 1.0f;
     if (MODE == MODE_GRAD && a.dloss != nullptr) weight *= a.dloss[t];
@@ -295,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             m = m2;
             if (i0 >= last) break;
             i0 += BATCH;
-            load(i0, MODE == MODE_STEP);
+            load(i0, MODE == MODE_STEP && i0 < last);
         }
         if (mine.edge >= 0) join(m, s, edge, edge == -INFINITY ? 0.0f : edge == edge ? 1.0f : edge, c);
 #pragma unroll
