@@ -440,19 +440,20 @@ int launch_rows(const DistillArgs& a, size_t rows, cudaStream_t st) {
     auto per = [&] { return (n + ((size_t)1 << pl) - 1) >> pl; };
     while (pl < 3 && (rows << (pl + 1)) <= 296 && per() > 512) ++pl;          // few rows: more blocks each
     if (MODE == MODE_GRAD) {
-        // nothing joins the parts: parts of 32 KB (4096 x 32768 bf16: 95 us, 99 in one part, 98 in four)
+        // nothing joins the parts: parts of 32 KB (4096 x 32768 bf16, before the arithmetic was packed: 95 us, 99 in one part, 98 in four)
         while (pl < 3 && per() > 2048) ++pl;
     }
     if (MODE != MODE_STEP) {
-        // rows up to 24 KB: smaller blocks, more rows on an SM (16384 x 8192 bf16, loss: 66 us with 64 threads, 71 with 128; from
-        // 64 KB on 101 and 97)
+        // Short rows want small blocks, many rows on an SM.  Loss, us with 64 / 128 / 256 threads: 16384 x 8192 bf16 53 / 60 / 107;
+        // 8192 x 32768 88 / 84 / 92; 2048 x 131072 89 / 87 / 84.  Gradient (parts of 32 KB at most): 92 / 101 / 121 and 169 / 165 / 189.
         if (per() <= 64 * 24) return launch_parts<T, 64, MODE>(a, rows, pl, per(), st);
-        return launch_parts<T, 128, MODE>(a, rows, pl, per(), st);
+        if (MODE == MODE_GRAD || per() < 64 * 128) return launch_parts<T, 128, MODE>(a, rows, pl, per(), st);
+        return launch_parts<T, 256, MODE>(a, rows, pl, per(), st);
     } else {
         // Few threads: many rows on an SM, but more batches between the first (shared memory) and the last (registers) that are
         // read twice; rows of up to 16 vectors a thread are read once.  Long rows re-read their middle, and from 256 KB on take two blocks, so that what is re-read is still
-        // in L2.  Measured, us with 64 / 128 / 256 / 512 threads: 16384 x 4099 fp32 104 / 122 / 172 / 298; 8192 x 32768 bf16
-        // 242 / 210 / 205 / 249; 4096 x 65536 268 / 235 / 203 / 213; 2048 x 131072 284 / 261 / 234 / 210.
+        // in L2.  Measured, us with 64 / 128 / 256 / 512 threads: 16384 x 4099 fp32 98 / 109 / 142 / 252; 8192 x 32768 bf16
+        // 223 / 189 / 189 / 206; 4096 x 65536 253 / 218 / 185 / 203; 2048 x 131072 270 / 246 / 215 / 193.
         while (pl < 3 && per() > 512 * 33) ++pl;
         if (per() <= 64 * 24) return launch_parts<T, 64, MODE>(a, rows, pl, per(), st);
         if (per() <= 128 * 24) return launch_parts<T, 128, MODE>(a, rows, pl, per(), st);
