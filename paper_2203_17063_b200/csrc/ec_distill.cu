@@ -252,6 +252,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
     __shared__ float s_p[MAX_TOP], s_z[MAX_TOP];
     __shared__ float2 s_stat[WARPS];                               // (maximum, sum) of each warp
     __shared__ Teacher s_teacher;
+    grid_dependency_wait();
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
     const int parts = 1 << parts_log2, part = (int)(blockIdx.x & (unsigned)(parts - 1));
     const size_t t = blockIdx.x >> parts_log2;
@@ -413,10 +414,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
 template <class T, int THREADS, int MODE>
 int launch_parts(const DistillArgs& a, size_t rows, int parts_log2, size_t vectors, cudaStream_t st) {
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1u << parts_log2; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = MODE != MODE_GRAD && parts_log2 > 0 ? 1 : 0; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = 1u << parts_log2; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = MODE != MODE_GRAD && parts_log2 > 0 ? 2 : 1; cfg.stream = st;
     cfg.gridDim = dim3((unsigned)(rows << parts_log2)); cfg.blockDim = dim3(THREADS);
     if (MODE == MODE_STEP && vectors > NV * THREADS) cfg.dynamicSmemBytes = NV * THREADS * 16;
     if (cfg.dynamicSmemBytes > 48 * 1024) {

@@ -27,6 +27,7 @@ template <class IDX, class TI, class TO, int W>
 __global__ void __launch_bounds__(LK_THREADS)
 lookup_kernel(const TI* __restrict__ table, size_t table_stride, size_t V, size_t D, const IDX* __restrict__ tokens, size_t T,
               float scale, TO* __restrict__ out, size_t out_stride) {
+    grid_dependency_wait();
     const int lane = threadIdx.x & 31;
     const size_t t = (size_t)blockIdx.x * (LK_THREADS / 32) + (threadIdx.x >> 5);
     if (t >= T) return;
@@ -75,8 +76,13 @@ int launch_lookup(const void* table, size_t V, size_t D, size_t ts, const void* 
     const size_t per = 32 * (size_t)u * LK_INFLIGHT, pieces = (D + per - 1) / per;
     const dim3 grid(gx, (unsigned)(pieces < 64 ? pieces : 64));
     auto launch = [&](auto kernel) {
-        kernel<<<grid, LK_THREADS, 0, st>>>((const TI*)table, ts, V, D, (const IDX*)tokens, T, scale, (TO*)out, os);
-        EC_CUDA(cudaGetLastError());
+        cudaLaunchConfig_t cfg = {};
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr; cfg.numAttrs = 1; cfg.stream = st;
+        cfg.gridDim = grid; cfg.blockDim = dim3(LK_THREADS);
+        EC_CUDA(cudaLaunchKernelEx(&cfg, kernel, (const TI*)table, ts, V, D, (const IDX*)tokens, T, scale, (TO*)out, os));
         return (int)EC_OK;
     };
     if constexpr (sizeof(TI) == 2) {

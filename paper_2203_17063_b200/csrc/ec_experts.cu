@@ -292,8 +292,6 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const uint32_t rank = PAIR ? blockIdx.x & 1u : 0u;
     const uint32_t worker = blockIdx.x / BLOCKS, workers = gridDim.x / BLOCKS;
     constexpr int tile_rows = MM_ROWS * BLOCKS;                // rows of a tile
-    if (!expert_ranges<mm_threads<TO>(MODE)>(a, tile_rows, s_row, s_tile, s_warp)) return;
-
     unsigned char* sm = mm_raw + ((1024u - (smem_u32(mm_raw) & 1023u)) & 1023u);
     auto out_buffer = [&](int w) { return sm + (size_t)pl.stages * pl.stage_bytes + w * (mm_out_bytes<TO>(MODE) / EPI); };
     const uint32_t stage0 = smem_u32(sm), bar0 = smem_u32(s_bar), nst = (uint32_t)pl.stages;
@@ -308,7 +306,16 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         s_abort = 0;
         mbar_init_fence();
     }
+    if (tid == 32) {
+        prefetch_map(&map_a);
+        prefetch_map(&map_b);
+    }
+    // What is above needs nothing of the launches before this one; it runs while the last of them drains.  The tensor memory
+    // is taken after the wait: a kernel that still runs, let go of its successor and only then takes its own would wait for
+    // this one, which waits for it.
+    grid_dependency_wait();
     if (warp == 2) tmem_alloc<PAIR>(smem_u32(&s_tmem), pl.tmem_cols);
+    const bool valid = expert_ranges<mm_threads<TO>(MODE)>(a, tile_rows, s_row, s_tile, s_warp);       // (all blocks see the same)
     fence_before_sync();
     __syncthreads();
     if (PAIR) cluster_sync();                                  // both blocks' barriers stand
@@ -318,8 +325,8 @@ expert_mma_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     // the tiles: for each expert, down the rows first
     const int cols = MODE == EX_FORWARD ? a.N : a.K, jt = (cols + pl.bn - 1) / pl.bn;
     const int wt = (a.N + MM_ROWS * BLOCKS - 1) / (MM_ROWS * BLOCKS);
-    const long long tiles = MODE == EX_WEIGHT ? (long long)a.E * wt * jt : (long long)s_tile[a.E] * jt;
-    if (MODE == EX_WEIGHT) {
+    const long long tiles = !valid ? 0 : MODE == EX_WEIGHT ? (long long)a.E * wt * jt : (long long)s_tile[a.E] * jt;
+    if (MODE == EX_WEIGHT && valid) {
         for (int e = tid; e < a.E; e += mm_threads<TO>(MODE)) {
             int at = e;
             if (a.E <= MM_SORT) {
@@ -597,10 +604,12 @@ int launch_mma(const ExpertArgs& a, int bn, int sms, cudaStream_t st) {
     const size_t most = MODE == EX_WEIGHT ? (size_t)a.E * ((a.N + MM_ROWS * BLOCKS - 1) / (MM_ROWS * BLOCKS)) * jt : (a.T / rows + a.E) * jt;
     const size_t workers = most < (size_t)sms / BLOCKS ? most : (size_t)sms / BLOCKS;
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = BLOCKS; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
-    cfg.attrs = attr; cfg.numAttrs = PAIR ? 1 : 0; cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = BLOCKS; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = PAIR ? 2 : 1; cfg.stream = st;
     cfg.gridDim = dim3((unsigned)(workers * BLOCKS)); cfg.blockDim = dim3(mm_threads<TO>(MODE)); cfg.dynamicSmemBytes = p.smem;
     EC_CUDA(cudaLaunchKernelEx(&cfg, expert_mma_kernel<TO, MODE, PAIR>, ma, mb, mo, a, p));
     return EC_OK;

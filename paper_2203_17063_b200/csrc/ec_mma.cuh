@@ -75,6 +75,9 @@ __device__ __forceinline__ void mbar_expect_tx_peer(uint32_t bar, uint32_t bytes
     asm volatile("mbarrier.arrive.expect_tx.relaxed.cluster.shared::cluster.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) {
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
+}
 // A load whose bytes are counted at `bar`: this block's barrier, or with PAIR one of the pair's (shared::cluster address).
 template <bool PAIR>
 __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
