@@ -18,6 +18,9 @@
 namespace ec {
 namespace {
 
+// The kernels here start while their predecessor in the stream still drains; what they read may be its results, so no pointer is
+// declared unaliased: the compiler would read it through the non-coherent path, whose lines the wait does not promise to renew.
+
 // ---- lookup ------------------------------------------------------------------------------------------------------
 
 constexpr int LK_THREADS = 256;
@@ -25,8 +28,8 @@ constexpr int LK_INFLIGHT = 4;          // vectors a lane has in flight
 
 template <class IDX, class TI, class TO, int W>
 __global__ void __launch_bounds__(LK_THREADS)
-lookup_kernel(const TI* __restrict__ table, size_t table_stride, size_t V, size_t D, const IDX* __restrict__ tokens, size_t T,
-              float scale, TO* __restrict__ out, size_t out_stride) {
+lookup_kernel(const TI* table, size_t table_stride, size_t V, size_t D, const IDX* tokens, size_t T,
+              float scale, TO* out, size_t out_stride) {
     grid_dependency_wait();
     const int lane = threadIdx.x & 31;
     const size_t t = (size_t)blockIdx.x * (LK_THREADS / 32) + (threadIdx.x >> 5);
@@ -425,7 +428,7 @@ struct GradArgs {
 // Where the border of a block at path step d lies: number of sorted tokens before it and row.  That is the tokens p with
 // p + key[p] < d, found by one warp, 33 sections at a time - moved back to a row's first token if the border falls between
 // two tokens of the row and fewer than GR_LONG of them lie before it, so that only long rows are cut and joined later.
-__device__ __forceinline__ void border(const uint32_t* __restrict__ keys, uint32_t T, uint32_t V, uint32_t d, int lane, uint32_t* tokens, uint32_t* row) {
+__device__ __forceinline__ void border(const uint32_t* keys, uint32_t T, uint32_t V, uint32_t d, int lane, uint32_t* tokens, uint32_t* row) {
     uint32_t lo = d > V ? d - V : 0u, hi = d < T ? d : T;
     while (lo < hi) {
         const uint32_t step = (hi - lo + 31) / 32, p = lo + lane * step;
@@ -484,7 +487,7 @@ __device__ __forceinline__ void write_unit(TO* p, const float* acc, float scale,
 // A block takes a stretch of the path: its rows without tokens are written with zeros by the warps in turn, its tokens are shared
 // out evenly to the groups.
 template <class TI, class TO, int U, int NU>
-__global__ void __launch_bounds__(GR_THREADS, 3) grad_walk_kernel(const GradArgs a, const TI* __restrict__ dout, TO* __restrict__ grad) {
+__global__ void __launch_bounds__(GR_THREADS, 3) grad_walk_kernel(const GradArgs a, const TI* dout, TO* grad) {
     grid_dependency_wait();
     __shared__ uint32_t s_key[GR_STEPS + GR_LONG + 2], s_pos[GR_STEPS + GR_LONG];      // s_key[0], s_key[n + 1]: the tokens before and behind the block's
     __shared__ uint32_t s_has[(GR_STEPS + GR_LONG) / 32 + 1];                          // bit r: row rows0 + r has tokens
@@ -649,7 +652,7 @@ __global__ void __launch_bounds__(GR_THREADS, 3) grad_walk_kernel(const GradArgs
 constexpr int JN_THREADS = 256, JN_WARPS = JN_THREADS / 32;
 
 template <class TO>
-__global__ void __launch_bounds__(JN_THREADS) grad_join_kernel(const GradArgs a, TO* __restrict__ grad) {
+__global__ void __launch_bounds__(JN_THREADS) grad_join_kernel(const GradArgs a, TO* grad) {
     grid_dependency_wait();
     __shared__ float s_part[JN_WARPS][128];
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
