@@ -11,8 +11,6 @@
 // fixed order.  The gradient is first written as if no entry were in the teacher's list; the list's entries follow behind a
 // barrier, each written by the block that owns its column.
 
-#include <atomic>
-
 #include "ec_vec.cuh"
 
 namespace ec {
@@ -422,15 +420,6 @@ int launch_parts(const DistillArgs& a, size_t rows, int parts_log2, size_t vecto
     cfg.attrs = attr; cfg.numAttrs = MODE != MODE_GRAD && parts_log2 > 0 ? 2 : 1; cfg.stream = st;
     cfg.gridDim = dim3((unsigned)(rows << parts_log2)); cfg.blockDim = dim3(THREADS);
     if (MODE == MODE_STEP && vectors > NV * THREADS) cfg.dynamicSmemBytes = NV * THREADS * 16;
-    if (cfg.dynamicSmemBytes > 48 * 1024) {
-        static std::atomic<uint64_t> ready{0};                     // devices on which the shared-memory limit is raised
-        int dev = 0;
-        EC_CUDA(cudaGetDevice(&dev));
-        if (dev >= 64 || !(ready.load(std::memory_order_relaxed) >> dev & 1u)) {
-            EC_CUDA(cudaFuncSetAttribute(distill_kernel<T, THREADS, MODE>, cudaFuncAttributeMaxDynamicSharedMemorySize, NV * THREADS * 16));
-            if (dev < 64) ready.fetch_or(1ull << dev, std::memory_order_relaxed);
-        }
-    }
     EC_CUDA(cudaLaunchKernelEx(&cfg, distill_kernel<T, THREADS, MODE>, a, parts_log2));
     return EC_OK;
 }
@@ -454,14 +443,15 @@ int launch_rows(const DistillArgs& a, size_t rows, cudaStream_t st) {
         return launch_parts<T, 256, MODE>(a, rows, pl, per(), st);
     } else {
         // Few threads: many rows on an SM, but more batches between the first (shared memory) and the last (registers) that are
-        // read twice; rows of up to 16 vectors a thread are read once.  Long rows re-read their middle, and from 256 KB on take two blocks, so that what is re-read is still
-        // in L2.  Measured, us with 64 / 128 / 256 / 512 threads: 16384 x 4099 fp32 98 / 109 / 142 / 252; 8192 x 32768 bf16
-        // 223 / 189 / 189 / 206; 4096 x 65536 253 / 218 / 185 / 203; 2048 x 131072 270 / 246 / 215 / 193.
-        while (pl < 3 && per() > 512 * 33) ++pl;
+        // read twice; rows of up to 16 vectors a thread are read once.  Measured, us with 64 / 128 / 256 threads: 16384 x 4099 fp32
+        // 98 / 109 / 142; 16384 x 16384 bf16 206 / 196 / 240; 8192 x 32768 223 / 189 / 195; 4096 x 65536 253 / 218 / 185.
+        // Longer rows take a cluster of such blocks rather than more threads: what is read twice has to be in L2 still, and four
+        // blocks an SM come out of step with each other.  us, one block of 512 threads / two of 256: 8192 x 131072 bf16 746 / 722,
+        // 2048 x 131072 193 / 192, 2048 x 100000 166 / 169; two / four: 2048 x 262144 393 / 379, 1024 x 131072 fp32 189 / 194.
+        while (pl < 3 && per() > 256 * 50) ++pl;
         if (per() <= 64 * 24) return launch_parts<T, 64, MODE>(a, rows, pl, per(), st);
         if (per() <= 128 * 24) return launch_parts<T, 128, MODE>(a, rows, pl, per(), st);
-        if (per() <= 256 * 40) return launch_parts<T, 256, MODE>(a, rows, pl, per(), st);
-        return launch_parts<T, 512, MODE>(a, rows, pl, per(), st);
+        return launch_parts<T, 256, MODE>(a, rows, pl, per(), st);
     }
 }
 
