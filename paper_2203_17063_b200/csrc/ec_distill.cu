@@ -5,11 +5,13 @@
 //   loss = w sum_k p_k (log p_k - u_{i_k} + lse)
 //   dz_v = g (m exp(u_v - lse) - sum over k with i_k = v of p_k),   m = sum_k p_k,  g = w / tau [* dloss]
 //
-// A row of logits is read once, its gradient written once: bound by memory.  Exponentials are taken to base 2: one fused
-// multiply-add and one ex2 an element, multiply-adds and additions two at a time (787 -> 756 us for 8192 x 131072 bf16).
-// Maxima, sums and the gradient are fp32, rounded once when the gradient is bf16.  Every thread keeps the maximum of what it has seen and the sum of exponentials below it; a block joins its threads in a
-// fixed order.  The gradient is first written as if no entry were in the teacher's list; the list's entries follow behind a
-// barrier, each written by the block that owns its column.
+// A row of logits is read once, its gradient written once: bound by memory, and under load by power (loss and gradient of
+// 8192 x 131072 bf16: 730 us on a cool GPU at 1965 MHz, 794 in a loop that runs into 1000 W at 1.7 GHz), so instructions count too.
+// Exponentials are taken to base 2: one fused multiply-add and one ex2 an element, multiply-adds and additions two at a time
+// (787 -> 756 us), a bf16 gradient's factor moved into the exponent (812 -> 794 in a loop).
+// Maxima, sums and the gradient are fp32, rounded once when the gradient is bf16.  Every thread keeps the maximum of what it has
+// seen and the sum of exponentials below it; a block joins its threads in a fixed order.  The gradient is first written as if no
+// entry were in the teacher's list; the list's entries follow behind a barrier, each written by the block that owns its column.
 
 #include "ec_vec.cuh"
 
@@ -345,7 +347,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
             G = g * mass / S;
         }
         if (skip) fused = false;
-        const f32x2 gg = pair(G, G), cc = pair(c, c), oo = pair(-off, -off);
+        // bf16: a positive G goes into the exponent (the sum's rounding, about 2^-24 of off - log2 G, is far below the result's; an
+        // fp32 gradient keeps the multiplication)
+        const bool in_exponent = sizeof(T) == 2 && fused && G >= 1e-30f && G <= 1e30f;
+        const float off2 = in_exponent ? off - log2f(G) : off;
+        const f32x2 gg = pair(G, G), cc = pair(c, c), oo = pair(-off2, -off2);
         auto scaled = [&](float x) {
             if (fused) return G * ex2(fmaf(x, c, -off));
             return G * ex2(MODE == MODE_GRAD ? fmaf(x, a.inv_tau, -lse) * LOG2E : (x - M) * c);
@@ -371,9 +377,12 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) distill_kernel(const 
                 if (i < mine.n) {
                     float x[W];
                     unpack<T, W>(v[q], x);
-                    if (fused) {
+                    if (sizeof(T) == 2 ? in_exponent : fused) {
 #pragma unroll
-                        for (int e = 0; e < W; e += 2) unpair(pair_mul(gg, pair_ex2(pair_fma(pair(x[e], x[e + 1]), cc, oo))), x[e], x[e + 1]);
+                        for (int e = 0; e < W; e += 2) {
+                            const f32x2 y = pair_ex2(pair_fma(pair(x[e], x[e + 1]), cc, oo));
+                            unpair(sizeof(T) == 2 ? y : pair_mul(gg, y), x[e], x[e + 1]);
+                        }
                     } else {
 #pragma unroll
                         for (int e = 0; e < W; ++e) x[e] = skip ? 0.0f : scaled(x[e]);
