@@ -151,6 +151,21 @@ def test_against_formulas(cuda_device, T, V, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,V,K", [(160, 110003, 6), (150, 210001, 40)])
+def test_many_long_rows(cuda_device, T, V, K, dtype):
+    """Rows that take several blocks for their length, not because there are few."""
+    z, i, l, w = problem(T, V, K, 31)
+    run_all(z.to(DT[dtype]), i, l, 1.5, w, None)
+
+
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e20, -3.0])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_weights_of_any_size(cuda_device, scale, dtype):
+    z, i, l, w = problem(12, 3001, 9, 32)
+    run_all(z.to(DT[dtype]), i, l, 2.0, w * scale, None, pad=3)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_gradient_rows_of_another_alignment(cuda_device, dtype):
     z, i, l, w = problem(7, 1003, 20, 1)
     run_all(z.to(DT[dtype]), i, l, 1.0, w, None, pad=1, offset=3, gpad=6, goffset=2)
