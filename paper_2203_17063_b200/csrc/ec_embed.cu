@@ -397,7 +397,7 @@ struct GradPlan {
 };
 
 // W: elements a thread takes of a row, as W / U units G units apart
-GradPlan grad_plan(size_t T, size_t V, size_t D, int U, int W) {
+GradPlan grad_plan(size_t steps, size_t D, int U, int W) {
     GradPlan p;
     p.U = U;
     const size_t lanes = (D + W - 1) / W;
@@ -405,8 +405,8 @@ GradPlan grad_plan(size_t T, size_t V, size_t D, int U, int W) {
     while (p.G < GR_THREADS && (size_t)p.G < lanes) p.G *= 2;
     p.slices = (unsigned)((lanes + p.G - 1) / p.G);
     const unsigned groups = GR_THREADS / p.G;
-    const size_t steps = T + V;
     p.C = GR_STEPS / (int)groups < GR_MAX_SHARE ? GR_STEPS / (int)groups : GR_MAX_SHARE;
+    // (12289 tokens on 50021 x 1001: 76 us; with half or twice as many blocks asked for 81 / 80)
     while (p.C > 8 && (steps / ((size_t)p.C * groups)) * p.slices < 148 * 8) p.C /= 2;
     p.blocks = (unsigned)((steps + (size_t)p.C * groups - 1) / ((size_t)p.C * groups));
     p.shares = p.blocks * groups;
@@ -428,8 +428,10 @@ struct GradArgs {
 // Where the border of a block at path step d lies: number of sorted tokens before it and row.  That is the tokens p with
 // p + key[p] < d, found by one warp, 33 sections at a time - moved back to a row's first token if the border falls between
 // two tokens of the row and fewer than GR_LONG of them lie before it, so that only long rows are cut and joined later.
-__device__ __forceinline__ void border(const uint32_t* keys, uint32_t T, uint32_t V, uint32_t d, int lane, uint32_t* tokens, uint32_t* row) {
-    uint32_t lo = d > V ? d - V : 0u, hi = d < T ? d : T;
+// A gradient that is added to what is there has no rows to fill with zeros: its path is the tokens alone, the border at token d
+// (4096 tokens on 65536 x 1024 fp32: 31 -> 23.5 us; 12289 on 50021 x 1001: 81 -> 75).
+__device__ __forceinline__ void border(const uint32_t* keys, uint32_t T, uint32_t V, bool rows, uint32_t d, int lane, uint32_t* tokens, uint32_t* row) {
+    uint32_t lo = !rows ? d : d > V ? d - V : 0u, hi = d < T ? d : T;
     while (lo < hi) {
         const uint32_t step = (hi - lo + 31) / 32, p = lo + lane * step;
         const bool less = p < hi && p + keys[p] < d;
@@ -439,7 +441,7 @@ __device__ __forceinline__ void border(const uint32_t* keys, uint32_t T, uint32_
         lo = lo + (n - 1) * step + 1;
         hi = top < hi ? top : hi;
     }
-    const uint32_t j = d - lo;
+    const uint32_t j = rows ? d - lo : lo < T ? keys[lo] : V;
     const uint32_t same = __ballot_sync(0xffffffffu, lo < T && lo > (uint32_t)lane && keys[lo] == j && keys[lo - 1 - lane] == j);
     static_assert(GR_LONG == 32, "one look back of a warp");
     *tokens = same == 0xffffffffu ? lo : lo - (uint32_t)(__ffs(~same) - 1);
@@ -493,11 +495,11 @@ __global__ void __launch_bounds__(GR_THREADS, 3) grad_walk_kernel(const GradArgs
     __shared__ uint32_t s_has[(GR_STEPS + GR_LONG) / 32 + 1];                          // bit r: row rows0 + r has tokens
     __shared__ uint32_t s_tok[2], s_rowat[2];
     const int tid = threadIdx.x, lane = tid & 31, w = tid >> 5;
-    const uint32_t groups = GR_THREADS / a.G, total = a.T + a.V;
+    const uint32_t groups = GR_THREADS / a.G, total = a.T + (a.accumulate ? 0u : a.V);
     const uint32_t d0 = blockIdx.x * groups * a.C, d1 = d0 + groups * a.C < total ? d0 + groups * a.C : total;
     if (w < 2) {
         uint32_t i, j;
-        border(a.keys, a.T, a.V, w == 0 ? d0 : d1, lane, &i, &j);
+        border(a.keys, a.T, a.V, !a.accumulate, w == 0 ? d0 : d1, lane, &i, &j);
         if (lane == 0) { s_tok[w] = i; s_rowat[w] = j; }
     } else {
         for (uint32_t q = tid - 64; q < sizeof(s_has) / 4; q += GR_THREADS - 64) s_has[q] = 0;
@@ -508,7 +510,7 @@ __global__ void __launch_bounds__(GR_THREADS, 3) grad_walk_kernel(const GradArgs
         const uint32_t k = i0 + q > 0 && i0 + q <= a.T ? a.keys[i0 + q - 1] : NO_ROW;
         s_key[q] = k;
         if (q > 0 && q <= n) s_pos[q - 1] = a.pos[i0 + q - 1];
-        if (k >= row0 && k < row1) atomicOr(&s_has[(k - row0) >> 5], 1u << ((k - row0) & 31));      // (bits: order is free)
+        if (!a.accumulate && k >= row0 && k < row1) atomicOr(&s_has[(k - row0) >> 5], 1u << ((k - row0) & 31));      // (bits: order is free)
     }
     __syncthreads();
 
@@ -717,8 +719,10 @@ void grad_layout(size_t T, size_t V, size_t D, GradLayout* L) {
     L->totals = off; off = align_up(off + SORT_BINS * 4, 256);
     size_t shares = 0;
     for (int W = 4; W <= 8; W += 4) {
-        const size_t n = grad_plan(T, V, D, 1, W).shares;
-        shares = n > shares ? n : shares;
+        for (size_t steps : {T, T + V}) {
+            const size_t n = steps == 0 ? 0 : grad_plan(steps, D, 1, W).shares;
+            shares = n > shares ? n : shares;
+        }
     }
     L->joins = off; off = align_up(off + (1 + 2 * shares) * 4, 256);
     L->begins = off; off = align_up(off + shares * 4, 256);
@@ -764,7 +768,7 @@ int sort_tokens(SortArgs a, const GradLayout& L, char* ws, cudaStream_t st) {
 template <class TI, class TO, int U>
 int launch_walk(GradArgs a, const void* dout, void* grad, cudaStream_t st) {
     constexpr int W = sizeof(TI) == 2 ? 8 : 4;
-    const GradPlan p = grad_plan(a.T, a.V, a.D, U, W);
+    const GradPlan p = grad_plan((size_t)a.T + (a.accumulate ? 0 : a.V), a.D, U, W);
     a.G = p.G;
     a.C = p.C;
     cudaLaunchConfig_t cfg = {};

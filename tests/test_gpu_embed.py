@@ -124,6 +124,24 @@ def test_grad(cuda_device, T, V, D, accumulate, src, dst):
             assert torch.equal(again, grad)
 
 
+@pytest.mark.parametrize("dst", ["f32", "bf16"])
+@pytest.mark.parametrize("off", [0, 1, 2, 3, 5, 7])
+@pytest.mark.parametrize("T,V,D", [(1, 4, 1), (9, 1003, 5), (250, 1000, 1024), (251, 1003, 1001), (900, 5000, 33)])
+def test_grad_of_few_tokens_without_gaps(cuda_device, T, V, D, off, dst):
+    """Rows that follow each other without gaps from any element on: nothing before or behind them is written."""
+    _, dout = make_rows(T, D, torch.float32, D, 41, offset=off)
+    g_all, grad = make_rows(V, D, DT[dst], D, 42, offset=off)
+    grad.fill_(float("inf"))
+    tokens = make_tokens("zipf", T, V, torch.int32, 43)
+    ws = torch.full((ec.embed_grad_workspace_bytes(T, V, D),), 0xA5, dtype=torch.uint8, device="cuda")
+    ec.embed_grad(dout, tokens, grad, ws, 0.5, -1, False)
+    torch.cuda.synchronize()
+    want, bound, _ = reference_grad(dout, tokens, V, 0.5, -1, None)
+    low, high = (want - bound).float().to(DT[dst]), (want + bound).float().to(DT[dst])
+    assert bool(((low <= grad) & (grad <= high)).all())
+    assert untouched(g_all, grad, D, off)
+
+
 @pytest.mark.parametrize("T,V,D,index", [(40000, 1000, 16, torch.int32), (65536, 70000, 8, torch.int64), (65537, 300, 24, torch.int64),
                                          (200001, 600000, 4, torch.int32), (150000, 3, 33, torch.int64)])
 def test_grad_of_many_tokens(cuda_device, T, V, D, index):
